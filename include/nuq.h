@@ -180,6 +180,110 @@ nuq_status nuq_decode_update(const void* const* streams, uint32_t K, uint64_t d,
                              float* acc, float* w, float* yl, float alpha, float mu, float l, void* stream);
 
 /*
+ * The optimizer's operators: AdamW (the paper trains with SGD and momentum, for which there is
+ * nuq_decode_update) over many tensors at once, the norm by which its gradients are clipped, and AdamW
+ * applied where the decoder finishes a sum.
+ *
+ * A tensor of n elements, contiguous.  Any alignment to its elements' size will do (parts of a decoded
+ * sum start anywhere); 16-byte aligned ones, or 8-byte ones of 16-bit and 4-byte ones of 8-bit elements,
+ * are moved with the widest loads.
+ *   types    NUQ_GRAD_*: what g holds; NUQ_COPY_*: what copy holds; NUQ_STATES_*: how m and v are kept
+ *   g        gradient; only read
+ *   w        fp32 parameters, updated in place
+ *   copy     NUQ_COPY_NONE: not looked at; else receives w rounded to nearest (the parameters that a
+ *            mixed-precision model computes with)
+ *   m, v     fp32 moments, updated in place (zeros before the first step); with NUQ_STATES_8BIT n bytes
+ *            each, and
+ *   scales   ceil(n / 256) pairs of floats, 8-byte aligned (else not looked at).  Block b of 256 elements
+ *            holds m = scales[2 b] e4m3(code of m) and sqrt(v) = scales[2 b + 1] e4m3(code of v): the root,
+ *            because it spans half as many powers of two.  A scale is the block's largest finite magnitude
+ *            (2^-100 at least) / 448.  Codes are rounded up or down with the probabilities that keep the
+ *            mean: with beta2 = 0.999 a step changes v by 0.1 % at most where it decays, and rounding to
+ *            the nearest of values that lie 6 to 12 % apart would undo every such change.  sqrt(v) > 0 is
+ *            never rounded to 0.  The element's step itself takes m and v before they are rounded.  A
+ *            value that is not finite is held as NaN (code 0x7f, 0xff), also where it was infinite.
+ *            All zeros (codes and scales) are the state before the first step.
+ *   weight_decay  of this tensor (0 for biases and the like)
+ * n = 0 is allowed (the pointers are not looked at then).  No two buffers that a call writes may overlap,
+ * nor may g with one of them.
+ */
+#define NUQ_GRAD_F32 0u
+#define NUQ_GRAD_BF16 1u
+#define NUQ_GRAD_F16 2u
+#define NUQ_COPY_NONE (0u << 8)
+#define NUQ_COPY_BF16 (1u << 8)
+#define NUQ_COPY_F16 (2u << 8)
+#define NUQ_STATES_F32 (0u << 16)
+#define NUQ_STATES_8BIT (1u << 16)
+#define NUQ_STATE_BLOCK 256u
+
+typedef struct nuq_tensor {
+    const void* g;
+    float* w;
+    void* copy;
+    void* m;
+    void* v;
+    float* scales;
+    uint64_t n;
+    float weight_decay;
+    uint32_t types;
+} nuq_tensor;
+
+/*
+ * What a step knows on the device, so that a captured step goes on counting, follows its schedule and is
+ * skipped when a gradient is not finite: a record of NUQ_CONTROL_BYTES in the caller's device memory,
+ * 16-byte aligned.  The caller fills it with zeros, sets step to the number of steps taken and lr_factor
+ * to 1; what lies behind the fields is scratch of nuq_grad_norm (a record serves one optimizer: calls that
+ * share it must be ordered).
+ */
+typedef struct nuq_control {
+    uint64_t step;           /* steps taken, the one that nuq_grad_norm has begun included          */
+    float norm;              /* out: |scale| times the gradients' Euclidean norm                    */
+    float scale;             /* out: what the step multiplies gradients by: scale min(1, max_norm / norm) */
+    float lr_factor;         /* the caller's: multiplies the learning rate                          */
+    uint32_t skip;           /* out: 1 when norm is not finite; steps with this record change nothing then */
+} nuq_control;
+#define NUQ_CONTROL_BYTES 16384u
+
+/*
+ * The Euclidean norm of all tensors' gradients together (g, n and types are looked at), and with it the
+ * step's beginning: writes norm, scale and skip of *control and adds 1 to its step unless skip is set.
+ *   tensors   HOST array of `count` tensors, copied at call time; any number, also none (norm 0: the step
+ *             begins without a norm)
+ *   scale     multiplies the gradients (1 / the loss's factor); finite
+ *   max_norm  > 0; infinity: no clipping
+ *   control   device
+ * Squares are added in fp32 by eights and beyond that in fp64, in an order that does not change, so equal
+ * gradients in the same tensors give the same bits on the same kind of GPU.  May be captured into a graph.
+ */
+nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale, float max_norm, nuq_control* control,
+                         void* stream);
+
+/*
+ * One AdamW step (decoupled weight decay) over all tensors:
+ *     g' = scale g,   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2,
+ *     w  = (1 - lr weight_decay) w - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * fp32 arithmetic; the factors are formed in fp64 and rounded once (with a control on the device in fp32).
+ *   tensors   HOST array, copied at call time; states of both kinds may be mixed
+ *   config    HOST; lr, weight_decay, eps >= 0 and finite, beta1 and beta2 in [0, 1), scale finite
+ *             step: t, from 1 on (not looked at with a control); seed: of the roundings of 8-bit states:
+ *             element i of tensor j (its place in the array) takes word i & 3 of Philox4x32-10(key = seed,
+ *             counter = (i >> 2 (two words), t, j)), the lower 16 bits for m, the upper ones for sqrt(v).
+ *   control   device, or NULL.  If given t is its step, gradients are multiplied by its scale too, lr by its
+ *             lr_factor; with skip set, or step 0, nothing is changed.
+ * Calls keep no state and use no workspace; they may be captured into graphs (a captured step without a
+ * control repeats the t of the capture) and run on several streams at once.
+ */
+typedef struct nuq_adamw_config {
+    double lr, beta1, beta2, eps;
+    double scale;
+    uint64_t step;
+    uint64_t seed;
+} nuq_adamw_config;
+nuq_status nuq_adamw(const nuq_tensor* tensors, uint32_t count, const nuq_adamw_config* config,
+                     const nuq_control* control, void* stream);
+
+/*
  * nuq_encode for callers that must not allocate device memory.  (The paper has
  * no counterpart; this entry point exists for deployment reasons only.)
  *

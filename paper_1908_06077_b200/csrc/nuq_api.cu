@@ -1,6 +1,8 @@
 // C ABI of the library (see include/nuq.h): argument validation, geometry,
 // per-stream workspace, kernel launches.  No torch types, no CPU fallback: every
 // step of the path runs in the kernels of nuq_encode.cu / nuq_decode_chains.cu.
+#include <math.h>
+
 #include <map>
 #include <mutex>
 #include <set>
@@ -674,6 +676,70 @@ nuq_status nuq_decode_update(const void* const* streams, uint32_t K, uint64_t d,
                              float* w, float* yl, float alpha, float mu, float l, void* stream) {
     if (!w) return NUQ_ERR_INVALID_ARG;
     return enqueue_decode(streams, K, d, bucket, s, acc, w, yl, alpha, mu, l, stream);
+}
+
+// What a list of tensors has to satisfy; `norm`: only its gradients are looked at.
+static bool tensors_ok(const nuq_tensor* tensors, uint32_t count, bool norm) {
+    if (count != 0u && !tensors) return false;
+    auto off = [](const void* p, uintptr_t unit) { return !p || (reinterpret_cast<uintptr_t>(p) & (unit - 1u)) != 0u; };
+    for (uint32_t i = 0; i < count; ++i) {
+        const nuq_tensor& t = tensors[i];
+        const uint32_t grad = t.types & 0xffu, copy = t.types & 0xff00u, states = t.types & 0xffff0000u;
+        if (grad > NUQ_GRAD_F16 || copy > NUQ_COPY_F16 || states > NUQ_STATES_8BIT || t.n >= (1ull << 40)) return false;
+        if (!norm && !(t.weight_decay >= 0.0f && t.weight_decay <= 3.4028234e38f)) return false;
+        if (t.n == 0u) continue;
+        if (off(t.g, grad == NUQ_GRAD_F32 ? 4u : 2u)) return false;
+        if (norm) continue;
+        if (off(t.w, 4u) || off(t.m, states == NUQ_STATES_8BIT ? 1u : 4u) || off(t.v, states == NUQ_STATES_8BIT ? 1u : 4u)) return false;
+        if ((copy != NUQ_COPY_NONE && off(t.copy, 2u)) || (states == NUQ_STATES_8BIT && off(t.scales, 8u))) return false;
+    }
+    return true;
+}
+
+nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale, float max_norm, nuq_control* control, void* stream) {
+    std::lock_guard<std::mutex> lock(g_mu);
+    if (!tensors_ok(tensors, count, true) || !control || (reinterpret_cast<uintptr_t>(control) & 15u)) return NUQ_ERR_INVALID_ARG;
+    if (!(scale >= -3.4028234e38f && scale <= 3.4028234e38f) || !(max_norm > 0.0f)) return NUQ_ERR_INVALID_ARG;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return NUQ_ERR_CUDA;
+    return launch_grad_norm(tensors, count, scale, max_norm, control, device_sms(dev), static_cast<cudaStream_t>(stream)) == cudaSuccess ? NUQ_OK : NUQ_ERR_CUDA;
+}
+
+// The step's constants: formed in fp64, rounded once.  False for arguments out of range.
+static bool make_adamw(const nuq_adamw_config* c, const nuq_control* control, double divisor, AdamwParams* P) {
+    const double most = 3.4028234e38;
+    if (!c || (reinterpret_cast<uintptr_t>(control) & 15u)) return false;
+    if (!(c->lr >= 0.0 && c->lr <= most) || !(c->eps >= 0.0 && c->eps <= most) || !(c->scale >= -most && c->scale <= most)) return false;
+    if (!(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0)) return false;
+    if (!control && c->step == 0u) return false;
+    P->lr = (float)c->lr;
+    P->beta1 = (float)c->beta1;
+    P->rest1 = (float)(1.0 - c->beta1);
+    P->beta2 = (float)c->beta2;
+    P->rest2 = (float)(1.0 - c->beta2);
+    P->eps = (float)c->eps;
+    P->scale = (float)(c->scale / divisor);
+    P->log1 = (float)log(c->beta1);
+    P->log2 = (float)log(c->beta2);
+    const double t = (double)(control ? 1u : c->step);
+    P->first = (float)(c->lr / -expm1(t * log(c->beta1)));
+    P->second = (float)(1.0 / sqrt(-expm1(t * log(c->beta2))));
+    P->t = (uint32_t)c->step;
+    P->control = control;
+    for (uint32_t r = 0; r < 10; ++r) {                     // Philox key schedule, as for the encoder
+        P->round_keys[2 * r] = (uint32_t)c->seed + r * 0x9E3779B9u;
+        P->round_keys[2 * r + 1] = (uint32_t)(c->seed >> 32) + r * 0xBB67AE85u;
+    }
+    return true;
+}
+
+nuq_status nuq_adamw(const nuq_tensor* tensors, uint32_t count, const nuq_adamw_config* config, const nuq_control* control, void* stream) {
+    std::lock_guard<std::mutex> lock(g_mu);
+    AdamwParams P;
+    if (!tensors_ok(tensors, count, false) || !make_adamw(config, control, 1.0, &P)) return NUQ_ERR_INVALID_ARG;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return NUQ_ERR_CUDA;
+    return launch_adamw(tensors, count, P, config->lr, device_sms(dev), static_cast<cudaStream_t>(stream)) == cudaSuccess ? NUQ_OK : NUQ_ERR_CUDA;
 }
 
 nuq_status nuq_last_status(void* stream_) {

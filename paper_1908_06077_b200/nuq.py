@@ -23,6 +23,11 @@ TEST_NORMS = 1 << 24
 TEST_SHORT_PATIENCE = 1 << 25
 HEADER_WORDS = 16
 STATIC_SCRATCH_BYTES = 512 * 1024
+GRAD_F32, GRAD_BF16, GRAD_F16 = 0, 1, 2
+COPY_NONE, COPY_BF16, COPY_F16 = 0 << 8, 1 << 8, 2 << 8
+STATES_F32, STATES_8BIT = 0 << 16, 1 << 16
+STATE_BLOCK = 256
+CONTROL_BYTES = 16384
 
 
 class NuqError(RuntimeError):
@@ -35,6 +40,16 @@ class _Info(C.Structure):
     _fields_ = [("d", C.c_uint64), ("bucket", C.c_uint32), ("s", C.c_uint32), ("flags", C.c_uint32),
                 ("sub_block", C.c_uint32), ("nblk", C.c_uint64), ("container_bits", C.c_uint64),
                 ("code_bits", C.c_uint64), ("nnz", C.c_uint64)]
+
+
+class _Tensor(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("w", C.c_void_p), ("copy", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("scales", C.c_void_p), ("n", C.c_uint64), ("weight_decay", C.c_float), ("types", C.c_uint32)]
+
+
+class _AdamwConfig(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("scale", C.c_double),
+                ("step", C.c_uint64), ("seed", C.c_uint64)]
 
 
 def _load():
@@ -53,6 +68,10 @@ def _load():
     lib.nuq_decode_update.restype = C.c_int
     lib.nuq_decode_update.argtypes = [C.POINTER(C.c_void_p), C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint32,
                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_float, C.c_float, C.c_void_p]
+    lib.nuq_grad_norm.restype = C.c_int
+    lib.nuq_grad_norm.argtypes = [C.c_void_p, C.c_uint32, C.c_float, C.c_float, C.c_void_p, C.c_void_p]
+    lib.nuq_adamw.restype = C.c_int
+    lib.nuq_adamw.argtypes = [C.c_void_p, C.c_uint32, C.POINTER(_AdamwConfig), C.c_void_p, C.c_void_p]
     lib.nuq_encode_bound.restype = C.c_uint64
     lib.nuq_encode_bound.argtypes = [C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32]
     lib.nuq_set_level_table.restype = C.c_int
@@ -215,6 +234,137 @@ def decode_update(streams, d, bucket, s, w, yl=None, alpha=1.0, mu=0.0, l=0.0, a
     if rc != NUQ_OK:
         raise NuqError("nuq_decode_update", rc)
     return w
+
+
+_GRADS = {torch.float32: GRAD_F32, torch.bfloat16: GRAD_BF16, torch.float16: GRAD_F16}
+_COPIES = {torch.bfloat16: COPY_BF16, torch.float16: COPY_F16}
+
+
+class Tensors:
+    """A list of tensors as grad_norm and adamw take it (see `tensors`).  It keeps the tensors alive; their contents are
+    looked at by the calls it is given to, so it serves step after step as long as the tensors stay where they are."""
+
+    def __init__(self, array, device, kept, states):
+        self.array, self.device, self.kept, self.states = array, device, kept, states
+
+    def __len__(self):
+        return len(self.array)
+
+
+def tensors(g, w=None, m=None, v=None, scales=None, copy=None, weight_decay=0.0) -> Tensors:
+    """The list of tensors for grad_norm (gradients alone) and adamw.
+
+    g     gradients: contiguous CUDA tensors of float32, bfloat16 or float16
+    w     parameters, float32, as many elements each
+    m, v  states: both float32, or both uint8 (codes) with `scales`, float32 of 2 * ceil(n / 256) elements
+    copy  bfloat16 or float16 copies of the parameters; the list or an entry may be None
+    weight_decay  one number, or one per tensor
+    Raises ValueError where shapes, types, devices or alignment do not fit, or where written memory is given twice."""
+    g = list(g)
+    count = len(g)
+    lists = {"w": w, "m": m, "v": v, "scales": scales, "copy": copy}
+    for name, x in lists.items():
+        x = lists[name] = [None] * count if x is None else list(x)
+        if len(x) != count:
+            raise ValueError(f"{name}: {len(x)} tensors for {count} gradients")
+    decays = [float(weight_decay)] * count if isinstance(weight_decay, (int, float)) else [float(x) for x in weight_decay]
+    if len(decays) != count:
+        raise ValueError(f"weight_decay: {len(decays)} numbers for {count} gradients")
+    states = w is not None
+    if not states and any(x is not None for x in (m, v, scales, copy)):
+        raise ValueError("states or copies without parameters")
+    array, device, written, read = (_Tensor * count)(), None, [], []
+
+    def place(name, i, x, types, n, out=True):
+        if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous() or x.dtype not in types or x.numel() != n:
+            raise ValueError(f"{name}[{i}]: a contiguous CUDA tensor of {n} elements, {' or '.join(map(str, types))}, is wanted")
+        if x.device != device:
+            raise ValueError(f"{name}[{i}]: on {x.device}, the first gradient is on {device}")
+        p = x.data_ptr()
+        if n:
+            (written if out else read).append((p, p + n * x.element_size(), f"{name}[{i}]"))
+        return p
+
+    for i, x in enumerate(g):
+        if device is None and isinstance(x, torch.Tensor):
+            device = x.device
+        n = x.numel() if isinstance(x, torch.Tensor) else 0
+        t = array[i]
+        t.g, t.n, t.weight_decay = place("g", i, x, tuple(_GRADS), n, False), n, decays[i]
+        t.types = _GRADS[x.dtype]
+        if not states:
+            continue
+        t.w = place("w", i, lists["w"][i], (torch.float32,), n)
+        t.m = place("m", i, lists["m"][i], (torch.float32, torch.uint8), n)
+        t.v = place("v", i, lists["v"][i], (lists["m"][i].dtype,), n)
+        if lists["m"][i].dtype == torch.uint8:
+            t.types |= STATES_8BIT
+            t.scales = place("scales", i, lists["scales"][i], (torch.float32,), 2 * -(-n // STATE_BLOCK))
+            if t.scales and t.scales % 8:
+                raise ValueError(f"scales[{i}]: 8-byte alignment is wanted")
+        if lists["copy"][i] is not None:
+            t.copy = place("copy", i, lists["copy"][i], tuple(_COPIES), n)
+            t.types |= _COPIES[lists["copy"][i].dtype]
+    ends = {True: (0, ""), False: (0, "")}                  # of what is written, of what is read (that may be given twice)
+    for a, b, name, writes in sorted([x + (True,) for x in written] + [x + (False,) for x in read]):
+        for end, other in (ends[True], ends[False] if writes else (0, "")):
+            if a < end:
+                raise ValueError(f"{name} and {other} overlap")
+        ends[writes] = max(ends[writes], (b, name))
+    return Tensors(array, device, (g, lists), states)
+
+
+def step_control(step=0, device=None) -> torch.Tensor:
+    """A step's record on the device (nuq_control): an int64 CUDA tensor, steps taken set to `step`, the learning rate's factor to 1."""
+    control = torch.zeros(CONTROL_BYTES // 8, dtype=torch.int64, device="cuda" if device is None else device)
+    control[0] = int(step)
+    control.view(torch.float32)[4] = 1.0
+    return control
+
+
+def control_fields(control) -> dict:
+    """The record's fields as views of it (CUDA tensors of one element): step, norm, scale, lr_factor, skip."""
+    f = control.view(torch.float32)
+    return {"step": control[0], "norm": f[2], "scale": f[3], "lr_factor": f[4], "skip": control.view(torch.int32)[5]}
+
+
+def _control(control, device):
+    if control is None:
+        return None
+    if not control.is_cuda or control.dtype != torch.int64 or not control.is_contiguous() or 8 * control.numel() < CONTROL_BYTES:
+        raise ValueError(f"control: a contiguous int64 CUDA tensor of {CONTROL_BYTES // 8} elements is wanted")
+    if device is not None and control.device != device:
+        raise ValueError(f"control: on {control.device}, the tensors are on {device}")
+    return control.data_ptr()
+
+
+def _on_device(device, stream, call):
+    """call(raw stream) with `device` current (the stream, if none is given, is its current one)"""
+    if device is None or device.index == _current_device():
+        return call(_stream(stream))
+    with torch.cuda.device(device):
+        return call(_stream(stream))
+
+
+def grad_norm(list_, control, max_norm=float("inf"), scale=1.0, stream=None):
+    """The gradients' Euclidean norm, the factor that clips it to max_norm and the beginning of the next step, all into
+    `control` (see control_fields).  list_: from `tensors`."""
+    where = _control(control, list_.device)
+    rc = _on_device(control.device, stream, lambda s: _lib.nuq_grad_norm(list_.array, len(list_), scale, max_norm, where, s))
+    if rc != NUQ_OK:
+        raise NuqError("nuq_grad_norm", rc)
+    return control
+
+
+def adamw(list_, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=0, scale=1.0, seed=0, control=None, stream=None):
+    """One AdamW step over the tensors of list_ (from `tensors`), in place.  step: its number, from 1 on, or `control`."""
+    if not list_.states:
+        raise ValueError("a list of gradients alone")
+    where = _control(control, list_.device)
+    config = _AdamwConfig(lr, beta1, beta2, eps, scale, step, seed)
+    rc = _on_device(list_.device, stream, lambda s: _lib.nuq_adamw(list_.array, len(list_), C.byref(config), where, s))
+    if rc != NUQ_OK:
+        raise NuqError("nuq_adamw", rc)
 
 
 def last_status(stream=None) -> int:
