@@ -265,7 +265,7 @@ nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale,
  *     w  = (1 - lr weight_decay) w - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * fp32 arithmetic; the factors are formed in fp64 and rounded once (with a control on the device in fp32).
  *   tensors   HOST array, copied at call time; states of both kinds may be mixed
- *   config    HOST; lr, weight_decay, eps >= 0 and finite, beta1 and beta2 in [0, 1), scale finite
+ *   config    HOST; lr, weight_decay >= 0 and finite, eps in [0, 2^100], beta1 and beta2 in [0, 1), scale finite
  *             step: t, from 1 on (not looked at with a control); seed: of the roundings of 8-bit states:
  *             element i of tensor j (its place in the array) takes word i & 3 of Philox4x32-10(key = seed,
  *             counter = (i >> 2 (two words), t, j)), the lower 16 bits for m, the upper ones for sqrt(v).
