@@ -119,8 +119,8 @@ typedef struct nuq_info {
  * The kernel is launched so that its blocks may be set up while the kernel
  * before it in the stream ends; it reads and writes memory only after that
  * kernel has ended, so the order of the stream holds for g, out, out_bits.
- * CUDA graphs: encode and decode calls (nuq_decode_accumulate, nuq_decode_update)
- * may be captured and replayed.  Arguments, level table and level code are those
+ * CUDA graphs: encode and decode calls (nuq_decode_accumulate, nuq_decode_update,
+ * nuq_decode_adamw) may be captured and replayed.  Arguments, level table and level code are those
  * of the capture; data are those in the buffers at the replay.  The encode
  * kernels leave the workspace as they found it, the decode kernels keep nothing
  * there but a latched error.  What a capture does not allow has to be done by a
@@ -282,6 +282,27 @@ typedef struct nuq_adamw_config {
 } nuq_adamw_config;
 nuq_status nuq_adamw(const nuq_tensor* tensors, uint32_t count, const nuq_adamw_config* config,
                      const nuq_control* control, void* stream);
+
+/*
+ * The aggregation line of Algorithm 1 fused into DECODE with an AdamW step in the place of the SGD one:
+ * g = (1 / K) sum_k DECODE(c_k) is the gradient of one tensor of d elements, whose step is nuq_adamw's with
+ * fp32 states.  The sum is not written out and read again, and decoding overlaps the step's memory traffic.
+ *
+ *   streams, K, d, bucket, s   as for nuq_decode_accumulate
+ *   likely   what the containers most likely are, as nuq_encode was told (NUQ_MODE_* | NUQ_LEVELS_*), or
+ *            NUQ_LIKELY_AS_KNOWN: what this process has encoded at their addresses, if anything.  Received
+ *            containers are not known.  It chooses the kernel; wrong, it costs time, not correctness.
+ *   acc      device, d floats, 16-byte aligned, or NULL: receives the sum as from nuq_decode_accumulate
+ *   w, m, v  device, d floats each, 16-byte aligned; updated in place; no two of them and acc may overlap
+ *   weight_decay, config, control   as for nuq_adamw (scale multiplies the mean; the seed is not looked at).
+ *            With a control whose skip is set w, m and v stay, acc is written all the same.
+ * Clipping by the norm needs the whole sum first: nuq_decode_accumulate, nuq_grad_norm, nuq_adamw.
+ * Errors and captures as for nuq_decode_update; the first call on a device uploads tables of its own.
+ */
+#define NUQ_LIKELY_AS_KNOWN 0xffffffffu
+nuq_status nuq_decode_adamw(const void* const* streams, uint32_t K, uint64_t d, uint32_t bucket, uint32_t s,
+                            uint32_t likely, float* acc, float* w, float* m, float* v, float weight_decay,
+                            const nuq_adamw_config* config, const nuq_control* control, void* stream);
 
 /*
  * nuq_encode for callers that must not allocate device memory.  (The paper has

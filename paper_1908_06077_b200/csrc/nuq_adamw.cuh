@@ -18,6 +18,14 @@ struct AdamwParams {
     uint32_t round_keys[20];                     // Philox4x32-10 key schedule of the seed, as in EncodeParams
 };
 
+// The decoder's sums applied at once: see SumParams.
+struct AdamwSum {
+    float* acc;              // where they are stored too, or nullptr
+    float *w, *m, *v;
+    float decay;             // lr weight_decay
+    AdamwParams step;
+};
+
 // The step is m / (root second / first + eps / first).
 struct AdamwFactors {
     float scale, root_factor, eps, lr_factor;

@@ -1,6 +1,6 @@
 // C ABI of the library (see include/nuq.h): argument validation, geometry,
 // per-stream workspace, kernel launches.  No torch types, no CPU fallback: every
-// step of the path runs in the kernels of nuq_encode.cu / nuq_decode_chains.cu.
+// step of the path runs in the kernels of nuq_encode.cu / nuq_decode_chains.cuh / nuq_adamw.cu.
 #include <math.h>
 
 #include <map>
@@ -40,7 +40,8 @@ std::mutex g_mu;
 std::map<std::pair<int, cudaStream_t>, WsEntry> g_ws;
 std::map<int, int> g_sms;                 // device -> SM count
 std::set<int> g_lut_ready;                // devices whose constant LUT is uploaded ...
-std::set<int> g_token_tables_ready;       // ... and those that hold the decoder's token tables
+std::set<int> g_token_tables_ready;       // ... and those that hold the decoder's token tables ...
+std::set<int> g_adamw_token_tables_ready; // ... and those of the decoder with the AdamW step
 std::map<int, const float*> g_test_norms;   // device -> bucket norms of nuq_set_test_norms
 float g_levels[kMaxTableS + 2], g_inv_width[kMaxTableS + 2];   // the level table of nuq_set_level_table ...
 uint32_t g_levels_s = 0;                                       // ... and its number of interior levels (0: none set)
@@ -604,20 +605,10 @@ nuq_status nuq_encode_static(const float* g, uint64_t d, uint32_t bucket, uint32
     return enqueue_encode(P, pl, g, norm_kind, seed, offset, out, out_bits, it->second, norms, nullptr, dev, stream);
 }
 
-// Shared by the two decode entry points.  `w` == nullptr: the sums only.
-static nuq_status enqueue_decode(const void* const* streams, uint32_t K, uint64_t d, uint32_t bucket, uint32_t s, float* acc,
-                                 float* w, float* yl, float alpha, float mu, float l, void* stream_) {
-    std::lock_guard<std::mutex> lock(g_mu);
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    DecodeParams P;
+// Shared by the decode entry points: the containers, what is likely of them, the stream's workspace.  P.sum is the caller's.
+static nuq_status prepare_decode(DecodeCall& P, const void* const* streams, uint32_t K, uint64_t d, uint32_t bucket, uint32_t s, uint32_t likely, cudaStream_t stream,
+                                 std::set<int>& tables_ready, cudaError_t (*upload)(), int* dev_out) {
     if (!streams || K < 1 || K > kMaxK) return NUQ_ERR_INVALID_ARG;
-    // (with one or two streams acc has to be given: a rule of the interface, which the kernels have no need of)
-    if (!acc && (!w || K < 3)) return NUQ_ERR_INVALID_ARG;
-    if (w && mu != 0.0f && !yl) return NUQ_ERR_INVALID_ARG;
-    if (w && !(alpha == alpha && mu >= 0.0f && mu < 1.0f && l >= 0.0f && l <= 1.0f)) return NUQ_ERR_INVALID_ARG;
-    if ((reinterpret_cast<uintptr_t>(acc) & 15u) || (reinterpret_cast<uintptr_t>(w) & 15u) ||
-        (reinterpret_cast<uintptr_t>(yl) & 15u))
-        return NUQ_ERR_INVALID_ARG;
     // the level set and mode come from each container's header; geometry only needs (d, bucket, s)
     if (!make_geometry(d, bucket, s, 0, &P.geo)) return NUQ_ERR_INVALID_ARG;
     for (uint32_t k = 0; k < K; ++k) {
@@ -628,9 +619,9 @@ static nuq_status enqueue_decode(const void* const* streams, uint32_t K, uint64_
     P.K = K;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return NUQ_ERR_CUDA;
-    if (!g_token_tables_ready.count(dev)) {
-        if (upload_token_tables() != cudaSuccess) return NUQ_ERR_CUDA;
-        g_token_tables_ready.insert(dev);
+    if (!tables_ready.count(dev)) {
+        if (upload() != cudaSuccess) return NUQ_ERR_CUDA;
+        tables_ready.insert(dev);
     }
     P.unit_subs = 0;                                    // (chosen at the launch)
     uint32_t fixed = 0, tokens = 0;                     // streams of each mode, as far as is known
@@ -638,8 +629,12 @@ static nuq_status enqueue_decode(const void* const* streams, uint32_t K, uint64_
     bool alike = true;
     for (uint32_t k = 0; k < K; ++k) {
         const auto it = g_container_mode.find(std::make_pair(dev, streams[k]));
-        const uint32_t mode = it == g_container_mode.end() ? kModeErc : it->second & 0xffu;
-        const uint32_t levels = it == g_container_mode.end() ? kLevelsExp : it->second >> 8;
+        uint32_t mode = it == g_container_mode.end() ? kModeErc : it->second & 0xffu;
+        uint32_t levels = it == g_container_mode.end() ? kLevelsExp : it->second >> 8;
+        if (likely != NUQ_LIKELY_AS_KNOWN) {
+            mode = (likely >> 16) & 0xffu;
+            levels = (likely >> 8) & 0xffu;
+        }
         fixed += mode == kModeFixed;
         tokens += mode == kModeErc;
         if (k == 0) P.likely_levels = levels;
@@ -650,20 +645,39 @@ static nuq_status enqueue_decode(const void* const* streams, uint32_t K, uint64_
     P.likely_table = kTabCoded;
     if (exists && fixed == K && alike) P.likely_table = kTabFields;
     else if (exists && tokens == K) P.likely_table = P.likely_levels == kLevelsUniform ? kTabUniform : kTabErc;
-    P.sum.acc = acc;
-    P.sum.w = w;
-    P.sum.yl = w && mu != 0.0f ? yl : nullptr;
-    P.sum.step_c = w ? (float)((double)alpha / (double)K) : 0.0f;          // one rounding each
-    P.sum.step_lc = w ? (float)((double)l * (double)alpha / (double)K) : 0.0f;
-    P.sum.mu = w ? mu : 0.0f;
     P.minus_zero = -0.0f;
     Workspace* ws = nullptr;
     nuq_status st = get_workspace(stream, sizeof(Workspace), &ws, &dev);
     if (st != NUQ_OK) return st;
     P.ws = ws;
     P.let_next = 0;                                     // (chosen at the launch, like unit_subs)
-    if (launch_decode(P, device_sms(dev), stream) != cudaSuccess) return NUQ_ERR_CUDA;
+    *dev_out = dev;
     return NUQ_OK;
+}
+
+// nuq_decode_accumulate and nuq_decode_update.  `w` == nullptr: the sums only.
+static nuq_status enqueue_decode(const void* const* streams, uint32_t K, uint64_t d, uint32_t bucket, uint32_t s, float* acc,
+                                 float* w, float* yl, float alpha, float mu, float l, void* stream_) {
+    std::lock_guard<std::mutex> lock(g_mu);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    DecodeParams P;
+    // (with one or two streams acc has to be given: a rule of the interface, which the kernels have no need of)
+    if (!acc && (!w || K < 3)) return NUQ_ERR_INVALID_ARG;
+    if (w && mu != 0.0f && !yl) return NUQ_ERR_INVALID_ARG;
+    if (w && !(alpha == alpha && mu >= 0.0f && mu < 1.0f && l >= 0.0f && l <= 1.0f)) return NUQ_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(acc) & 15u) || (reinterpret_cast<uintptr_t>(w) & 15u) ||
+        (reinterpret_cast<uintptr_t>(yl) & 15u))
+        return NUQ_ERR_INVALID_ARG;
+    int dev = 0;
+    const nuq_status st = prepare_decode(P, streams, K, d, bucket, s, NUQ_LIKELY_AS_KNOWN, stream, g_token_tables_ready, upload_token_tables, &dev);
+    if (st != NUQ_OK) return st;
+    P.sum.acc = acc;
+    P.sum.w = w;
+    P.sum.yl = w && mu != 0.0f ? yl : nullptr;
+    P.sum.step_c = w ? (float)((double)alpha / (double)K) : 0.0f;          // one rounding each
+    P.sum.step_lc = w ? (float)((double)l * (double)alpha / (double)K) : 0.0f;
+    P.sum.mu = w ? mu : 0.0f;
+    return launch_decode(P, device_sms(dev), stream) == cudaSuccess ? NUQ_OK : NUQ_ERR_CUDA;
 }
 
 nuq_status nuq_decode_accumulate(const void* const* streams, uint32_t K, uint64_t d, uint32_t bucket, uint32_t s,
@@ -740,6 +754,27 @@ nuq_status nuq_adamw(const nuq_tensor* tensors, uint32_t count, const nuq_adamw_
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return NUQ_ERR_CUDA;
     return launch_adamw(tensors, count, P, config->lr, device_sms(dev), static_cast<cudaStream_t>(stream)) == cudaSuccess ? NUQ_OK : NUQ_ERR_CUDA;
+}
+
+nuq_status nuq_decode_adamw(const void* const* streams, uint32_t K, uint64_t d, uint32_t bucket, uint32_t s, uint32_t likely, float* acc, float* w, float* m, float* v,
+                            float weight_decay, const nuq_adamw_config* config, const nuq_control* control, void* stream_) {
+    std::lock_guard<std::mutex> lock(g_mu);
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_);
+    auto off = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0u; };
+    if (!w || !m || !v || off(w) || off(m) || off(v) || off(acc)) return NUQ_ERR_INVALID_ARG;
+    if (!(weight_decay >= 0.0f && weight_decay <= 3.4028234e38f)) return NUQ_ERR_INVALID_ARG;
+    if (likely != NUQ_LIKELY_AS_KNOWN && ((likely & 0xff0000ffu) != 0u || ((likely >> 8) & 0xffu) > kLevelsTable || (likely >> 16) > kModeCoded)) return NUQ_ERR_INVALID_ARG;
+    DecodeParamsOf<AdamwSum> P;
+    if (K < 1 || !make_adamw(config, control, (double)K, &P.sum.step)) return NUQ_ERR_INVALID_ARG;
+    int dev = 0;
+    const nuq_status st = prepare_decode(P, streams, K, d, bucket, s, likely, stream, g_adamw_token_tables_ready, upload_adamw_token_tables, &dev);
+    if (st != NUQ_OK) return st;
+    P.sum.acc = acc;
+    P.sum.w = w;
+    P.sum.m = m;
+    P.sum.v = v;
+    P.sum.decay = (float)(config->lr * (double)weight_decay);
+    return launch_decode_adamw(P, device_sms(dev), stream) == cudaSuccess ? NUQ_OK : NUQ_ERR_CUDA;
 }
 
 nuq_status nuq_last_status(void* stream_) {

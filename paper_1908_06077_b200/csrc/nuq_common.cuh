@@ -106,18 +106,24 @@ struct SumParams {
     float mu;
 };
 
-struct DecodeParams {
+struct DecodeCall {
     Geometry geo;
-    SumParams sum;
     const uint32_t* streams[kMaxK];
     uint32_t K;
     uint32_t unit_subs;      // token streams: sub-blocks a warp decodes at a time
     uint32_t likely_table;   // the table the call most likely needs (kTabErc, kTabUniform, kTabFields), or kTabCoded: none to prepare (a level code of the streams' own, or streams of several kinds)
     uint32_t likely_levels;  // ... and the level set of its fields (kTabFields)
     uint32_t let_next;       // token streams: the kernel behind may be launched early
-    float minus_zero;        // -0.0f, which the compiler must not know (see product2 in nuq_decode_common.cuh)
+    float minus_zero;        // -0.0f, which the compiler must not know (see product2 in nuq_pairs.cuh)
     Workspace* ws;
 };
+// Sum: SumParams, or AdamwSum of nuq_adamw.cuh
+template <class Sum>
+struct DecodeParamsOf : DecodeCall {
+    using SumType = Sum;
+    Sum sum;
+};
+using DecodeParams = DecodeParamsOf<SumParams>;
 
 __device__ __forceinline__ void latch_status(Workspace* ws, int code) {
     if (code > 0) atomicCAS(&ws->status, 0, code);          // a warning never hides an error

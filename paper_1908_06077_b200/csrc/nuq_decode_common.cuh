@@ -1,6 +1,7 @@
 // Shared by the decode kernels: what a container's header says (checked on the device), the value of a symbol,
 // and what happens to the finished sum of an element (stored, or applied to the parameters at once).
 #pragma once
+#include "nuq_adamw.cuh"
 #include "nuq_common.cuh"
 #include "nuq_pairs.cuh"
 
@@ -32,9 +33,25 @@ __device__ __forceinline__ float step_value(const SumParams& P, float w, float G
     *yl = yl_next;
     return w_next;
 }
-// element e (a multiple of 4) and the three behind it, with the parameters and y^l as they were
-__device__ __forceinline__ void step4(const SumParams& P, uint64_t e, float4 G, float4 w, float4 yl) {
+// What the step reads, asked for some time before it is needed: so many vectors of parameters, from these addresses on.
+__device__ __forceinline__ uint32_t step_vectors(const SumParams& P) { return P.w == nullptr ? 0u : P.mu != 0.0f ? 2u : 1u; }
+__device__ __forceinline__ const float* step_vector(const SumParams& P, uint32_t i) { return i == 0u ? P.w : P.yl; }
+__device__ __forceinline__ bool stores_only(const SumParams& P) { return P.w == nullptr; }
+__device__ __forceinline__ void begin_step(const SumParams&) {}
+// the parameters and y^l of element e (a multiple of 4) and the three behind it, as they were
+struct Held {
+    float4 w, yl;
+};
+__device__ __forceinline__ Held no_step4(const SumParams&) { return {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}; }
+__device__ __forceinline__ Held load_step4(const SumParams& P, uint64_t e) {
+    Held h;
+    h.w = *reinterpret_cast<const float4*>(P.w + e);
+    h.yl = P.mu != 0.0f ? *reinterpret_cast<const float4*>(P.yl + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+    return h;
+}
+__device__ __forceinline__ void step4(const SumParams& P, uint64_t e, float4 G, Held h) {
     if (P.acc) *reinterpret_cast<float4*>(P.acc + e) = G;
+    float4 w = h.w, yl = h.yl;
     w.x = step_value(P, w.x, G.x, &yl.x);
     w.y = step_value(P, w.y, G.y, &yl.y);
     w.z = step_value(P, w.z, G.z, &yl.z);
@@ -43,14 +60,8 @@ __device__ __forceinline__ void step4(const SumParams& P, uint64_t e, float4 G, 
     if (P.mu != 0.0f) *reinterpret_cast<float4*>(P.yl + e) = yl;
 }
 __device__ __forceinline__ void finish4(const SumParams& P, uint64_t e, float4 G) {
-    if (!P.w) {
-        *reinterpret_cast<float4*>(P.acc + e) = G;
-        return;
-    }
-    float4 yl = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float4 w = *reinterpret_cast<const float4*>(P.w + e);
-    if (P.mu != 0.0f) yl = *reinterpret_cast<const float4*>(P.yl + e);
-    step4(P, e, G, w, yl);
+    if (!P.w) *reinterpret_cast<float4*>(P.acc + e) = G;
+    else step4(P, e, G, load_step4(P, e));
 }
 __device__ __forceinline__ void finish1(const SumParams& P, uint64_t e, float G) {
     if (P.acc) P.acc[e] = G;
@@ -61,8 +72,58 @@ __device__ __forceinline__ void finish1(const SumParams& P, uint64_t e, float G)
     }
 }
 
+// The same for the AdamW step (the mean of the streams is in its scale; no acc is needed).  Its factors are taken once per CTA, by the
+// thread that calls begin_step; the others meet it before they need them.
+__device__ __forceinline__ AdamwFactors& step_factors() {
+    __shared__ AdamwFactors f;
+    return f;
+}
+__device__ __forceinline__ uint32_t step_vectors(const AdamwSum&) { return 3u; }
+__device__ __forceinline__ const float* step_vector(const AdamwSum& P, uint32_t i) { return i == 0u ? P.w : i == 1u ? P.m : P.v; }
+__device__ __forceinline__ bool stores_only(const AdamwSum&) { return false; }
+__device__ __forceinline__ void begin_step(const AdamwSum& P) {
+    AdamwFactors f = adamw_factors(P.step);
+    f.lr_factor = 1.0f - f.lr_factor * P.decay;             // (what multiplies w)
+    step_factors() = f;
+}
+struct AdamwHeld {
+    float4 w, m, v;
+};
+__device__ __forceinline__ AdamwHeld no_step4(const AdamwSum&) {
+    const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+    return {z, z, z};
+}
+__device__ __forceinline__ AdamwHeld load_step4(const AdamwSum& P, uint64_t e) {
+    return {*reinterpret_cast<const float4*>(P.w + e), *reinterpret_cast<const float4*>(P.m + e), *reinterpret_cast<const float4*>(P.v + e)};
+}
+__device__ __forceinline__ void adamw_step(const AdamwSum& P, const AdamwFactors& f, float G, float& w, float& m, float& v) {
+    const float g = __fmul_rn(G, f.scale);
+    m = moment1(P.step, g, m);
+    v = moment2(P.step, g, v);
+    w = adamw_value(f, f.lr_factor, w, m, __fsqrt_rn(v));
+}
+__device__ __forceinline__ void step4(const AdamwSum& P, uint64_t e, float4 G, AdamwHeld h) {
+    if (P.acc) *reinterpret_cast<float4*>(P.acc + e) = G;
+    const AdamwFactors f = step_factors();
+    if (!f.taken) return;
+    adamw_step(P, f, G.x, h.w.x, h.m.x, h.v.x);
+    adamw_step(P, f, G.y, h.w.y, h.m.y, h.v.y);
+    adamw_step(P, f, G.z, h.w.z, h.m.z, h.v.z);
+    adamw_step(P, f, G.w, h.w.w, h.m.w, h.v.w);
+    *reinterpret_cast<float4*>(P.w + e) = h.w;
+    *reinterpret_cast<float4*>(P.m + e) = h.m;
+    *reinterpret_cast<float4*>(P.v + e) = h.v;
+}
+__device__ __forceinline__ void finish4(const AdamwSum& P, uint64_t e, float4 G) { step4(P, e, G, load_step4(P, e)); }
+__device__ __forceinline__ void finish1(const AdamwSum& P, uint64_t e, float G) {
+    if (P.acc) P.acc[e] = G;
+    const AdamwFactors f = step_factors();
+    if (f.taken) adamw_step(P, f, G, P.w[e], P.m[e], P.v[e]);
+}
+
 // the first n < 4 elements from e on
-__device__ __forceinline__ void finish_part(const SumParams& P, uint64_t e, float4 G, uint32_t n) {
+template <class Sum>
+__device__ __forceinline__ void finish_part(const Sum& P, uint64_t e, float4 G, uint32_t n) {
     if (n > 0u) finish1(P, e, G.x);
     if (n > 1u) finish1(P, e + 1, G.y);
     if (n > 2u) finish1(P, e + 2, G.z);

@@ -1,5 +1,5 @@
 // DECODE + aggregate of calls whose streams are all in the fixed-width mode with the same field width and kind of levels:
-// no chains to walk.  The kernels for it, and the way here from the kernels for token streams, are in nuq_decode_chains.cu.
+// no chains to walk.  The kernels for it, and the way here from the kernels for token streams, are in nuq_decode_chains.cuh.
 //
 // A warp takes units of up to four 256-element sub-blocks; a lane has eight consecutive elements of each, one word of
 // every stream when fields have 4 bits.  A field, its sign bit included, is looked up in a table of level values in shared
@@ -37,7 +37,7 @@ __host__ __device__ constexpr uint32_t field_table_stride(uint32_t w) { return w
 
 // The level values by field; a symbol that does not exist stands for NaN, which the sums keep (and are checked for).
 // `heads`: of the n streams whose own levels they are (level tables).
-__device__ __noinline__ void build_field_tables(const Geometry& G, uint32_t levelset, const StreamHead* heads, uint32_t n, unsigned char* tables) {
+static __device__ __noinline__ void build_field_tables(const Geometry& G, uint32_t levelset, const StreamHead* heads, uint32_t n, unsigned char* tables) {
     const uint32_t nlev = level_count(levelset, G.s), w = field_width(nlev), stride = field_table_stride(w);
     for (uint32_t i = threadIdx.x; i < n << w; i += blockDim.x) {
         const uint32_t k = i >> w, f = i & ((1u << w) - 1u), sym = f & ((1u << (w - 1u)) - 1u);
@@ -87,7 +87,7 @@ __device__ __forceinline__ void eight_levels(const uint32_t (&x)[field_words(W)]
 
 // Four fields of a fixed-width stream, elements e .. e + 3 of the vector (e a multiple of 4), as values.  Returns
 // false when a symbol does not exist.
-__device__ __noinline__ bool four_fields(const Geometry& G, const StreamHead& hd, uint64_t e, float4* out) {
+static __device__ __noinline__ bool four_fields(const Geometry& G, const StreamHead& hd, uint64_t e, float4* out) {
     const uint32_t wd = hd.width, smask = (1u << (wd - 1u)) - 1u;
     const uint64_t b = e / G.bucket;
     const uint32_t in_bucket = (uint32_t)(e - b * G.bucket), rec_words = 1u + (G.bucket * wd + 31u) / 32u;
@@ -116,7 +116,8 @@ __device__ __noinline__ bool four_fields(const Geometry& G, const StreamHead& hd
 // ones, and four warps per scheduler wait for instructions as much as for data (check_fields alone: 56.0 -> 52.3 us).
 
 // A lane's elements (e0 + 256 q + 0 .. 7) of a unit with norms that are not all of ordinary size, from the containers.
-__device__ __noinline__ void unit_slowly(const DecodeParams& P, const StreamHead* heads, uint64_t e0, uint32_t slots) {
+template <class Params>
+__device__ __noinline__ void unit_slowly(const Params& P, const StreamHead* heads, uint64_t e0, uint32_t slots) {
     bool ok = true;
 #pragma unroll 1
     for (uint32_t i = 0; i < 2u * slots; ++i) {
@@ -136,7 +137,7 @@ __device__ __noinline__ void unit_slowly(const DecodeParams& P, const StreamHead
 }
 
 // Looks for symbols that do not exist among a lane's elements.
-__device__ __noinline__ void check_fields(const DecodeParams& P, const StreamHead* heads, uint64_t e0, uint32_t slots) {
+static __device__ __noinline__ void check_fields(const DecodeCall& P, const StreamHead* heads, uint64_t e0, uint32_t slots) {
     bool ok = true;
     for (uint32_t i = 0; i < 2u * slots; ++i) {
         const uint64_t e = e0 + kSB * (i / 2u) + 4u * (i & 1u);
@@ -149,8 +150,8 @@ __device__ __noinline__ void check_fields(const DecodeParams& P, const StreamHea
 }
 
 // The sums of a unit that reaches behind the vector's end.
-template <uint32_t SLOTS>
-__device__ __forceinline__ void finish_end(const SumParams& P, uint64_t d, uint64_t e0, uint32_t slots, const float (&sum)[SLOTS][8]) {
+template <uint32_t SLOTS, class Sum>
+__device__ __forceinline__ void finish_end(const Sum& P, uint64_t d, uint64_t e0, uint32_t slots, const float (&sum)[SLOTS][8]) {
     float v[8u * SLOTS];                                    // (a copy that can be indexed)
 #pragma unroll
     for (uint32_t i = 0; i < 8u * SLOTS; ++i) v[i] = sum[i / 8u][i % 8u];
@@ -176,8 +177,8 @@ __device__ __forceinline__ void store8(float* dst, const float (&v)[8]) {
 // element without a symbol has no product) take the slow way.
 // `mine`: the warp's shared memory (a multiple of 16).  `tables_ready`: the table of levels has been built, and all threads
 // have met since.
-template <uint32_t W, bool EXACT>
-__device__ __forceinline__ void decode_fields(const DecodeParams& P, const StreamHead* heads, unsigned char* table_memory, bool tables_ready, uint32_t mine) {
+template <uint32_t W, bool EXACT, class Params>
+__device__ __forceinline__ void decode_fields(const Params& P, const StreamHead* heads, unsigned char* table_memory, bool tables_ready, uint32_t mine) {
     constexpr uint32_t kWords = field_words(W), kSlots = field_slots(W), kPitch = field_pitch(W), kItem = kFieldStreams * kPitch;
     const Geometry& G = P.geo;
     const uint32_t lane = lane_id(), K = P.K, spb = G.bucket / kSB, rec_words = 1u + G.bucket * W / 32u, hwords = heads[0].hwords;
@@ -261,7 +262,7 @@ __device__ __forceinline__ void decode_fields(const DecodeParams& P, const Strea
     const bool wide = (reinterpret_cast<uintptr_t>(P.sum.acc) & 31u) == 0;
     float sum[kSlots][8];
     bool ordinary = true;                                   // so far, all norms of the unit
-    const uint32_t params = P.sum.w == nullptr ? 0u : P.sum.mu != 0.0f ? 2u : 1u;        // vectors of parameters
+    const uint32_t params = step_vectors(P.sum);            // vectors of parameters
     auto clear = [&] {
 #pragma unroll
         for (uint32_t i = 0; i < 8u * kSlots; ++i) sum[i / 8u][i % 8u] = 0.0f;
@@ -273,7 +274,7 @@ __device__ __forceinline__ void decode_fields(const DecodeParams& P, const Strea
         const uint64_t e0 = (uint64_t)sub * kSB + 8u * lane;
         if (n >= 2u) {
             if (cur.k0 == 0u && sub + slots <= nfull && lane < params)    // the parameters, for later
-                asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"((lane == 0u ? P.sum.w : P.sum.yl) + (uint64_t)sub * kSB), "r"(4u * kSB * slots) : "memory");
+                asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(step_vector(P.sum, lane) + (uint64_t)sub * kSB), "r"(4u * kSB * slots) : "memory");
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             const float norm = lane / kFieldStreams < slots && lane % kFieldStreams < count ? __uint_as_float(field_word(norms + 128u * stage + 4u * lane)) : 0.0f;
             const bool fine = EXACT ? norm == 0.0f || (norm >= 0x1p-100f && norm < 0x1p126f) : fabsf(norm) <= 3.4028234e38f;
@@ -317,7 +318,7 @@ __device__ __forceinline__ void decode_fields(const DecodeParams& P, const Strea
             __syncthreads();
         }
         if (n >= 2u && cur.k0 + kFieldStreams >= K) {       // the sums are complete
-            const SumParams out = P.sum;
+            const typename Params::SumType out = P.sum;
             float check = 0.0f;                             // NaN when a sum is not finite
 #pragma unroll
             for (uint32_t i = 0; i < 8u * kSlots; ++i) check = __fmaf_rn(sum[i / 8u][i % 8u], 0.0f, check);
@@ -328,7 +329,7 @@ __device__ __forceinline__ void decode_fields(const DecodeParams& P, const Strea
                 unit_slowly(P, heads, e0, slots);
             } else if (__builtin_expect(sub + slots > nfull, 0)) {
                 finish_end<kSlots>(out, G.d, e0, slots, sum);
-            } else if (out.w == nullptr) {
+            } else if (stores_only(out)) {
 #pragma unroll
                 for (uint32_t q = 0; q < kSlots; ++q) {
                     if (q >= slots) break;
@@ -343,19 +344,15 @@ __device__ __forceinline__ void decode_fields(const DecodeParams& P, const Strea
             } else {
 #pragma unroll
                 for (uint32_t i0 = 0; i0 < 2u * kSlots; i0 += 4u) {            // the loads of two slots are on their way together
-                    float4 w[4], yl[4];
+                    decltype(load_step4(out, 0)) held[4];
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i) {
-                        const uint64_t e = e0 + kSB * ((i0 + i) / 2u) + 4u * (i & 1u);
-                        w[i] = yl[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if ((i0 + i) / 2u < slots) {
-                            w[i] = *reinterpret_cast<const float4*>(out.w + e);
-                            if (out.mu != 0.0f) yl[i] = *reinterpret_cast<const float4*>(out.yl + e);
-                        }
+                        held[i] = no_step4(out);
+                        if ((i0 + i) / 2u < slots) held[i] = load_step4(out, e0 + kSB * ((i0 + i) / 2u) + 4u * (i & 1u));
                     }
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i)
-                        if ((i0 + i) / 2u < slots) step4(out, e0 + kSB * ((i0 + i) / 2u) + 4u * (i & 1u), value((i0 + i) / 2u, i & 1u), w[i], yl[i]);
+                        if ((i0 + i) / 2u < slots) step4(out, e0 + kSB * ((i0 + i) / 2u) + 4u * (i & 1u), value((i0 + i) / 2u, i & 1u), held[i]);
                 }
             }
             if (__builtin_expect(ordinary && !(check == 0.0f), 0)) check_fields(P, heads, e0, slots);   // a symbol that does not exist?
@@ -373,8 +370,8 @@ __device__ __forceinline__ void decode_fields(const DecodeParams& P, const Strea
 // instruction cache.  Kernel: a type of the calling kernel's own, so that each has a function for itself.  (In one that several
 // kernels called, built by nvcc 12.9, store8 wrote its first element only, in all kernels but one.  The source has no reason for
 // that: the same text is right where it is inlined and where one kernel calls it.)
-template <uint32_t W, bool EXACT, class Kernel>
-__device__ __noinline__ void decode_fields_call(const DecodeParams& P, const StreamHead* heads, unsigned char* table_memory, uint32_t mine) {
+template <uint32_t W, bool EXACT, class Kernel, class Params>
+__device__ __noinline__ void decode_fields_call(const Params& P, const StreamHead* heads, unsigned char* table_memory, uint32_t mine) {
     decode_fields<W, EXACT>(P, heads, table_memory, false, mine);
 }
 

@@ -43,6 +43,8 @@ cudaError_t launch_encode_fixed4(const EncodeParams& P, cudaStream_t stream);
 cudaError_t launch_level_histogram(const EncodeParams& P, uint64_t* hist, int sms, cudaStream_t stream);   // hist: s + 2 zeroed counters
 cudaError_t upload_token_tables();                    // the chain decoder's tables, likewise
 cudaError_t launch_decode(const DecodeParams& P, int sms, cudaStream_t stream);
+cudaError_t upload_adamw_token_tables();              // the same for the decoder with the AdamW step, which has its own
+cudaError_t launch_decode_adamw(const DecodeParamsOf<AdamwSum>& P, int sms, cudaStream_t stream);
 // `lr` of the decay only (P has the others): the tensors' weight_decay comes with it
 cudaError_t launch_adamw(const nuq_tensor* tensors, uint32_t count, const AdamwParams& P, double lr, int sms, cudaStream_t stream);
 cudaError_t launch_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale, float max_norm, nuq_control* control, int sms, cudaStream_t stream);

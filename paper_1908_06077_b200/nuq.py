@@ -28,6 +28,7 @@ COPY_NONE, COPY_BF16, COPY_F16 = 0 << 8, 1 << 8, 2 << 8
 STATES_F32, STATES_8BIT = 0 << 16, 1 << 16
 STATE_BLOCK = 256
 CONTROL_BYTES = 16384
+LIKELY_AS_KNOWN = 0xFFFFFFFF
 
 
 class NuqError(RuntimeError):
@@ -72,6 +73,10 @@ def _load():
     lib.nuq_grad_norm.argtypes = [C.c_void_p, C.c_uint32, C.c_float, C.c_float, C.c_void_p, C.c_void_p]
     lib.nuq_adamw.restype = C.c_int
     lib.nuq_adamw.argtypes = [C.c_void_p, C.c_uint32, C.POINTER(_AdamwConfig), C.c_void_p, C.c_void_p]
+    lib.nuq_decode_adamw.restype = C.c_int
+    lib.nuq_decode_adamw.argtypes = [C.POINTER(C.c_void_p), C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.POINTER(_AdamwConfig),
+                                     C.c_void_p, C.c_void_p]
     lib.nuq_encode_bound.restype = C.c_uint64
     lib.nuq_encode_bound.argtypes = [C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32]
     lib.nuq_set_level_table.restype = C.c_int
@@ -365,6 +370,28 @@ def adamw(list_, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=0, scale=1.0, seed=0
     rc = _on_device(list_.device, stream, lambda s: _lib.nuq_adamw(list_.array, len(list_), C.byref(config), where, s))
     if rc != NUQ_OK:
         raise NuqError("nuq_adamw", rc)
+
+
+def decode_adamw(streams, d, bucket, s, w, m, v, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=0, scale=1.0,
+                 control=None, likely=LIKELY_AS_KNOWN, acc=None, stream=None):
+    """An AdamW step with the mean of DECODE(streams[k]) as the gradient; w, m and v (float32, d elements) in place.
+    step: its number, from 1 on, or `control`.  likely: what the streams most likely are, as encode was told (MODE_* | LEVELS_*);
+    received containers are not known by their addresses."""
+    for name, x in (("w", w), ("m", m), ("v", v), ("acc", acc)):
+        if x is not None and not (x.is_cuda and x.dtype == torch.float32 and x.is_contiguous() and x.numel() == d and x.device == w.device):
+            raise ValueError(f"{name}: a contiguous float32 CUDA tensor of {d} elements is wanted, all on one device")
+    places = sorted((x.data_ptr(), x.data_ptr() + 4 * d) for x in (w, m, v, acc) if x is not None)
+    if any(a[1] > b[0] for a, b in zip(places, places[1:])):
+        raise ValueError("w, m, v and acc overlap")
+    where = _control(control, w.device)
+    config = _AdamwConfig(lr, beta1, beta2, eps, scale, step, 0)
+    ptrs = _pointers(streams)
+    rc = _on_device(w.device, stream, lambda raw: _lib.nuq_decode_adamw(
+        ptrs, len(streams), d, bucket, s, likely, acc.data_ptr() if acc is not None else None, w.data_ptr(), m.data_ptr(),
+        v.data_ptr(), weight_decay, C.byref(config), where, raw))
+    if rc != NUQ_OK:
+        raise NuqError("nuq_decode_adamw", rc)
+    return w
 
 
 def last_status(stream=None) -> int:

@@ -166,3 +166,38 @@ def test_the_reference_s_random_bits_are_philox():
     for q, row in zip((0, 5, (3 << 32) + 7), got):
         want = oracle.philox4x32_10([q & 0xFFFFFFFF, q >> 32, 11, 2], [seed & 0xFFFFFFFF, seed >> 32])
         assert list(row) == list(want)
+
+
+# ---- the decoder with the step ----
+
+def _decode(lib, K=3, d=100_000, bucket=1024, s=4, likely=0xFFFFFFFF, acc=None, w=W, m=M, v=V, decay=0.1, config=None, control=None, streams=None):
+    lib.nuq_decode_adamw.argtypes = [C.POINTER(C.c_void_p), C.c_uint32, C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_float, C.POINTER(Config), C.c_void_p, C.c_void_p]
+    array = (C.c_void_p * max(1, K))(*(streams or [0x2000] * max(1, K)))
+    return lib.nuq_decode_adamw(array, K, d, bucket, s, likely, acc, w, m, v, decay, config or _config(), control, STREAM)
+
+
+@pytest.mark.parametrize("kw", [dict(K=0), dict(K=65), dict(d=0), dict(d=1 << 40), dict(bucket=1000), dict(s=0), dict(s=15), dict(w=None), dict(m=None), dict(v=None),
+                                dict(w=W + 4), dict(m=M + 8), dict(v=V + 4), dict(acc=G + 4), dict(decay=-1.0), dict(decay=NAN), dict(likely=3 << 16), dict(likely=3 << 8),
+                                dict(likely=1), dict(likely=1 << 24), dict(config=_config(step=0)), dict(config=_config(lr=NAN)), dict(config=_config(scale=INF)),
+                                dict(control=CONTROL + 4), dict(streams=[0x2000, None, 0x2000]), dict(streams=[0x2000, 0x2008, 0x2000])])
+def test_decode_adamw_refuses(lib, kw):
+    assert _decode(lib, **kw) == -1
+    assert not _launches(lib)
+
+
+@pytest.mark.parametrize("likely,kernel", [(0, "decode_chains_kernel"), (1 << 16, "decode_fields_kernel"), (2 << 16, "decode_chains_kernel"), (1 << 16 | 1 << 8, "decode_chains_kernel"),
+                                           (0xFFFFFFFF, "decode_chains_kernel")])
+def test_decode_adamw_takes_the_likely_kernel(lib, likely, kernel):
+    for K in (1, 2, 3, 40):                                 # (the sum is needed by nobody, however many streams there are)
+        assert _decode(lib, K=K, likely=likely) == 0
+    assert len(_launches(lib)) == 4 and all(kernel in e and "AdamwSum" in e and e.endswith("unordered 0") for e in _launches(lib))
+
+
+def test_decode_adamw_in_a_capture_needs_a_call_before(lib):
+    lib.fake_capture(1)
+    assert _decode(lib) == -4
+    lib.fake_capture(0)
+    assert _decode(lib) == 0
+    lib.fake_capture(1)
+    assert _decode(lib, control=CONTROL, config=_config(step=0)) == 0
