@@ -447,10 +447,11 @@ enum : int { kStates32 = 0, kStates8 = 1, kStates8Narrow = 2 };
 template <uint32_t CAP, int KIND>
 __global__ void __launch_bounds__(kStepThreads, KIND != kStates32 ? kStepCtas8 : kStepCtas32) adamw_kernel(const __grid_constant__ StepTable<CAP> T, const __grid_constant__ AdamwParams P, const uint32_t rounds) {
     constexpr bool BITS8 = KIND != kStates32;
-    const AdamwFactors f = adamw_factors(P);
-    if (!f.taken) return;
     const uint32_t tile = blockIdx.x, i = tensor_of(T, tile, 0u);
     const StepTensor t = T.tensor[i];
+    asm volatile("griddepcontrol.wait;" ::: "memory");      // nothing before it reads or writes memory: see launch_overlapped
+    const AdamwFactors f = adamw_factors(P);
+    if (!f.taken) return;
     uint64_t e0 = (uint64_t)(tile - T.first[i]) * (kStepTile * rounds) + (threadIdx.x >> 5) * NUQ_STATE_BLOCK;
     const float keep = 1.0f - f.lr_factor * t.decay;
     __shared__ Staged s_staged[BITS8 ? kStepThreads / 32u : 1u];
@@ -480,10 +481,25 @@ __global__ void __launch_bounds__(kStepThreads, KIND != kStates32 ? kStepCtas8 :
     }
 }
 
+// Launches a kernel so that its CTAs may be set up while the kernel before it in the stream ends, if that one lets it in (the norm lets
+// the step in; the step, whose CTAs come and go, nobody).
+template <class... Params, class... Args>
+static cudaError_t launch_overlapped(void (*kernel)(Params...), uint32_t grid, uint32_t threads, cudaStream_t stream, const Args&... args) {
+    cudaLaunchConfig_t cfg = cudaLaunchConfig_t{};
+    cudaLaunchAttribute attr[1];
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 template <uint32_t CAP, int KIND>
 static cudaError_t launch_step(const StepTable<CAP>& T, const AdamwParams& P, uint32_t rounds, cudaStream_t stream) {
-    adamw_kernel<CAP, KIND><<<T.tiles, kStepThreads, 0, stream>>>(T, P, rounds);
-    return cudaGetLastError();
+    return launch_overlapped(adamw_kernel<CAP, KIND>, T.tiles, kStepThreads, stream, T, P, rounds);
 }
 
 constexpr uint32_t kStepMany = 400;                         // tensors of a launch: what fits the parameters
@@ -668,6 +684,8 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
                                                                   uint32_t begin, uint32_t end) {
     __shared__ double shared[kNormThreads / 32];
     __shared__ bool s_last;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     double sum = 0.0;
     uint32_t at = 0, end_tile = 0;                          // the tile's tensor, the tile behind its last
     for (uint32_t tile = blockIdx.x; tile < T.tiles; tile += gridDim.x) {
@@ -718,8 +736,7 @@ static cudaError_t launch_norm(const NormTable<kNormMany>& all, ControlRecord* c
     uint32_t grid = (uint32_t)sms * 8u;
     if (grid > kNormMaxGrid) grid = kNormMaxGrid;
     if (grid > T.tiles) grid = T.tiles ? T.tiles : 1u;
-    grad_norm_kernel<CAP><<<grid, kNormThreads, 0, stream>>>(T, control, scale, max_norm, begin, end);
-    return cudaGetLastError();
+    return launch_overlapped(grad_norm_kernel<CAP>, grid, kNormThreads, stream, T, control, scale, max_norm, (uint32_t)begin, (uint32_t)end);
 }
 
 cudaError_t launch_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale, float max_norm, nuq_control* control, int sms, cudaStream_t stream) {

@@ -77,6 +77,12 @@ __device__ __forceinline__ float ordinary_root(float v) {
     const float s = __fmul_rn(v, y);
     return __fmaf_rn(__fmaf_rn(-s, s, v), __fmul_rn(y, 0.5f), s);
 }
+// sqrt(v) within two units of its last place, for all v: where nothing but the step depends on it.
+__device__ __forceinline__ float root_estimate(float v) {
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(v));
+    return y;
+}
 __device__ __forceinline__ float reciprocal_estimate(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -89,10 +89,6 @@ __device__ __forceinline__ void begin_step(const AdamwSum& P) {
 struct AdamwHeld {
     float4 w, m, v;
 };
-__device__ __forceinline__ AdamwHeld no_step4(const AdamwSum&) {
-    const float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
-    return {z, z, z};
-}
 __device__ __forceinline__ AdamwHeld load_step4(const AdamwSum& P, uint64_t e) {
     return {*reinterpret_cast<const float4*>(P.w + e), *reinterpret_cast<const float4*>(P.m + e), *reinterpret_cast<const float4*>(P.v + e)};
 }
@@ -100,7 +96,7 @@ __device__ __forceinline__ void adamw_step(const AdamwSum& P, const AdamwFactors
     const float g = __fmul_rn(G, f.scale);
     m = moment1(P.step, g, m);
     v = moment2(P.step, g, v);
-    w = adamw_value(f, f.lr_factor, w, m, __fsqrt_rn(v));
+    w = adamw_value(f, f.lr_factor, w, m, root_estimate(v));
 }
 __device__ __forceinline__ void step4(const AdamwSum& P, uint64_t e, float4 G, AdamwHeld h) {
     if (P.acc) *reinterpret_cast<float4*>(P.acc + e) = G;

@@ -172,6 +172,52 @@ __device__ __forceinline__ void store8(float* dst, const float (&v)[8]) {
                  : "memory");
 }
 
+__device__ __forceinline__ void load8(float (&v)[8], const float* src) {
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(src));
+}
+// A lane's eight elements of the AdamW step.  wide: all arrays are at multiples of 32 bytes, so that whole sectors are moved (25.6 x 10^6
+// elements, K = 8, 4 bits: 123 us; in halves of sectors 137).
+struct Held8 {
+    float w[8], m[8], v[8];
+};
+__device__ __forceinline__ bool wide_step(const SumParams&) { return false; }
+__device__ __forceinline__ bool wide_step(const AdamwSum& P) {
+    return ((reinterpret_cast<uintptr_t>(P.w) | reinterpret_cast<uintptr_t>(P.m) | reinterpret_cast<uintptr_t>(P.v) | reinterpret_cast<uintptr_t>(P.acc)) & 31u) == 0;
+}
+__device__ __forceinline__ void get8(float (&x)[8], const float* p, bool wide) {
+    if (wide) {
+        load8(x, p);
+    } else {
+        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+}
+__device__ __forceinline__ void put8(float* p, const float (&x)[8], bool wide) {
+    if (wide) {
+        store8(p, x);
+    } else {
+        *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+    }
+}
+__device__ __forceinline__ Held8 load_step8(const AdamwSum& P, uint64_t e, bool wide) {
+    Held8 h;
+    get8(h.w, P.w + e, wide);
+    get8(h.m, P.m + e, wide);
+    get8(h.v, P.v + e, wide);
+    return h;
+}
+__device__ __forceinline__ void step8(const AdamwSum& P, uint64_t e, const float (&G)[8], Held8& h, bool wide) {
+    if (P.acc) put8(P.acc + e, G, wide);
+    const AdamwFactors f = step_factors();
+    if (!f.taken) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) adamw_step(P, f, G[i], h.w[i], h.m[i], h.v[i]);
+    put8(P.w + e, h.w, wide);
+    put8(P.m + e, h.m, wide);
+    put8(P.v + e, h.v, wide);
+}
+
 // EXACT: powers of two, whose product with a norm of ordinary size is exact, so that one fused operation gives the sum
 // that two would; else product and sum are rounded one after the other.  Other norms (tiny ones; not finite ones, where an
 // element without a symbol has no product) take the slow way.
@@ -260,9 +306,11 @@ __device__ __forceinline__ void decode_fields(const Params& P, const StreamHead*
     after.b = after.unit * S / spb;
     after.in = after.unit * S - after.b * spb;
     const bool wide = (reinterpret_cast<uintptr_t>(P.sum.acc) & 31u) == 0;
+    const bool wide_states = wide_step(P.sum);
     float sum[kSlots][8];
     bool ordinary = true;                                   // so far, all norms of the unit
     const uint32_t params = step_vectors(P.sum);            // vectors of parameters
+    constexpr bool kAdamw = std::is_same<typename Params::SumType, AdamwSum>::value;
     auto clear = [&] {
 #pragma unroll
         for (uint32_t i = 0; i < 8u * kSlots; ++i) sum[i / 8u][i % 8u] = 0.0f;
@@ -340,6 +388,17 @@ __device__ __forceinline__ void decode_fields(const Params& P, const StreamHead*
                         *reinterpret_cast<float4*>(dst) = value(q, 0u);
                         *reinterpret_cast<float4*>(dst + 4) = value(q, 1u);
                     }
+                }
+            } else if constexpr (kAdamw) {
+#pragma unroll
+                for (uint32_t q0 = 0; q0 < kSlots; q0 += 2u) {                 // the loads of two slots are on their way together
+                    Held8 held[2] = {};
+#pragma unroll
+                    for (uint32_t i = 0; i < 2; ++i)
+                        if (q0 + i < slots) held[i] = load_step8(out, e0 + kSB * (q0 + i), wide_states);
+#pragma unroll
+                    for (uint32_t i = 0; i < 2; ++i)
+                        if (q0 + i < slots) step8(out, e0 + kSB * (q0 + i), sum[q0 + i], held[i], wide_states);
                 }
             } else {
 #pragma unroll
