@@ -203,7 +203,7 @@ nuq_status nuq_decode_update(const void* const* streams, uint32_t K, uint64_t d,
  *            never rounded to 0.  The element's step itself takes m and v before they are rounded.  A
  *            value that is not finite is held as NaN (code 0x7f, 0xff), also where it was infinite.
  *            All zeros (codes and scales) are the state before the first step.
- *   weight_decay  of this tensor (0 for biases and the like)
+ *   weight_decay  of this tensor (0 for biases and the like), >= 0 and finite
  * n = 0 is allowed (the pointers are not looked at then).  No two buffers that a call writes may overlap,
  * nor may g with one of them.
  */
@@ -264,8 +264,10 @@ nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale,
  *     g' = scale g,   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2,
  *     w  = (1 - lr weight_decay) w - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * fp32 arithmetic; the factors are formed in fp64 and rounded once (with a control on the device in fp32).
+ * The quotient is m / (sqrt(v) a + b) with a and b formed beforehand, by an estimate of the reciprocal: within
+ * a few units of its last place; a denominator below 2^-126 counts as 0.
  *   tensors   HOST array, copied at call time; states of both kinds may be mixed
- *   config    HOST; lr, weight_decay >= 0 and finite, eps in [0, 2^100], beta1 and beta2 in [0, 1), scale finite
+ *   config    HOST; lr in [0, 2^40], eps in [0, 2^100], beta1 and beta2 in [0, 1), scale finite
  *             step: t, from 1 on (not looked at with a control); seed: of the roundings of 8-bit states:
  *             element i of tensor j (its place in the array) takes word i & 3 of Philox4x32-10(key = seed,
  *             counter = (i >> 2 (two words), t, j)), the lower 16 bits for m, the upper ones for sqrt(v).

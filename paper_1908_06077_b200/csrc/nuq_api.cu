@@ -723,7 +723,7 @@ nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale,
 static bool make_adamw(const nuq_adamw_config* c, const nuq_control* control, double divisor, AdamwParams* P) {
     const double most = 3.4028234e38;
     if (!c || (reinterpret_cast<uintptr_t>(control) & 15u)) return false;
-    if (!(c->lr >= 0.0 && c->lr <= most) || !(c->eps >= 0.0 && c->eps <= 0x1p100) || !(c->scale >= -most && c->scale <= most)) return false;
+    if (!(c->lr >= 0.0 && c->lr <= 0x1p40) || !(c->eps >= 0.0 && c->eps <= 0x1p100) || !(c->scale >= -most && c->scale <= most)) return false;
     if (!(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0)) return false;
     if (!control && c->step == 0u) return false;
     P->beta1 = (float)c->beta1;

@@ -343,6 +343,12 @@ def _control(control, device):
     return control.data_ptr()
 
 
+def _config(lr, beta1, beta2, eps, scale, step, seed):
+    if not 0 <= step < 1 << 64:                             # (ctypes would take what is left of it)
+        raise ValueError(f"step: {step}")
+    return _AdamwConfig(lr, beta1, beta2, eps, scale, step, seed & 0xFFFFFFFFFFFFFFFF)
+
+
 def _on_device(device, stream, call):
     """call(raw stream) with `device` current (the stream, if none is given, is its current one)"""
     if device is None or device.index == _current_device():
@@ -366,7 +372,7 @@ def adamw(list_, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=0, scale=1.0, seed=0
     if not list_.states:
         raise ValueError("a list of gradients alone")
     where = _control(control, list_.device)
-    config = _AdamwConfig(lr, beta1, beta2, eps, scale, step, seed)
+    config = _config(lr, beta1, beta2, eps, scale, step, seed)
     rc = _on_device(list_.device, stream, lambda s: _lib.nuq_adamw(list_.array, len(list_), C.byref(config), where, s))
     if rc != NUQ_OK:
         raise NuqError("nuq_adamw", rc)
@@ -384,7 +390,7 @@ def decode_adamw(streams, d, bucket, s, w, m, v, lr, beta1=0.9, beta2=0.999, eps
     if any(a[1] > b[0] for a, b in zip(places, places[1:])):
         raise ValueError("w, m, v and acc overlap")
     where = _control(control, w.device)
-    config = _AdamwConfig(lr, beta1, beta2, eps, scale, step, 0)
+    config = _config(lr, beta1, beta2, eps, scale, step, 0)
     ptrs = _pointers(streams)
     rc = _on_device(w.device, stream, lambda raw: _lib.nuq_decode_adamw(
         ptrs, len(streams), d, bucket, s, likely, acc.data_ptr() if acc is not None else None, w.data_ptr(), m.data_ptr(),

@@ -70,7 +70,7 @@ def _copy_bound(copy, w):
     return np.abs(w) * (2.0 ** -8 if copy == "bfloat16" else 2.0 ** -11) + 2.0 ** -25
 
 
-def _check(before, after, decays, t, bits, scale=1.0, copy=None, seed=0, lr=R.LR, beta1=R.BETA1, beta2=R.BETA2, eps=R.EPS):
+def _check(before, after, decays, t, bits, scale=1.0, copy=None, seed=0, lr=R.LR, beta1=R.BETA1, beta2=R.BETA2, eps=R.EPS, first=0):
     """every array of every tensor against the 64-bit step from what the device held before; returns how many codes were undecided"""
     undecided = total = 0
     for j, (a, b, decay) in enumerate(zip(before, after, decays)):
@@ -92,7 +92,7 @@ def _check(before, after, decays, t, bits, scale=1.0, copy=None, seed=0, lr=R.LR
             continue
         if n == 0:
             continue
-        words = R.philox(np.arange(-(-n // 4)), t, j, seed).reshape(-1)[:n].astype(np.int64)
+        words = R.philox(np.arange(-(-n // 4)) + first // 4, t, j, seed).reshape(-1)[:n].astype(np.int64)
         root, droot = np.sqrt(v), dv / (2.0 * np.sqrt(np.maximum(v, 1e-300))) + R.U * np.sqrt(v)
         for name, x, dx, random, k in (("m", m, dm, words & 0xFFFF, 0), ("v", root, droot, words >> 16, 1)):
             most = R.largest(x)
@@ -479,6 +479,41 @@ def test_encoded_decoded_clipped_and_applied():
     _check(before, after, [0.01] * len(sizes), 1, 32, f["scale"].item())
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_offsets_beyond_32_bits(bits):
+    """a tensor of more than 2^32 elements: the elements on both sides of 2^32 and the last ones, and the norm of all"""
+    torch, nuq = require_cuda()
+    n = (1 << 32) + 4099
+    need = n * (14 if bits == 32 else 8) + (4 << 30)
+    if torch.cuda.mem_get_info()[0] < need:
+        pytest.skip("not enough memory free")
+    rng = np.random.default_rng(3)
+    g, w = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, device="cuda")
+    dtype = torch.float32 if bits == 32 else torch.uint8
+    m, v = torch.zeros(n, dtype=dtype, device="cuda"), torch.zeros(n, dtype=dtype, device="cuda")
+    blocks = -(-n // R.BLOCK)
+    scales = torch.full((2 * blocks,), 1.0 / 448.0, device="cuda") if bits == 8 else None
+    # whole blocks each: the random bits go by an element's place, so the reference gets the places in front as if they were there
+    parts = [slice(0, 512), slice((1 << 31) - 512, (1 << 31) + 512), slice((1 << 32) - 512, (1 << 32) + 1024), slice((1 << 32) + 3840, n)]
+    for p in parts:
+        k = p.stop - p.start
+        g[p] = torch.from_numpy(rng.standard_normal(k).astype(np.float32)).cuda().to(torch.bfloat16)
+        w[p] = torch.from_numpy(rng.standard_normal(k).astype(np.float32)).cuda()
+        for x in (m, v):
+            x[p] = torch.from_numpy((rng.random(k) if bits == 32 else rng.integers(1, 126, k)).astype(np.float32)).cuda().to(dtype)
+    read = lambda: [{**{name: x[p].float().cpu().numpy() if x.dtype != torch.uint8 else x[p].cpu().numpy() for name, x in (("g", g), ("w", w), ("m", m), ("v", v))},  # noqa: E731
+                     **({"scales": scales[2 * (p.start // 256):2 * -(-p.stop // 256)].cpu().numpy()} if bits == 8 else {})} for p in parts]
+    before = read()
+    lst = nuq.tensors([g], [w], [m], [v], scales=[scales] if bits == 8 else None, weight_decay=0.1)
+    control = nuq.step_control(2)
+    nuq.grad_norm(lst, control, scale=1.0)
+    want = np.sqrt(sum((x["g"].astype(np.float64) ** 2).sum() for x in before))
+    assert abs(nuq.control_fields(control)["norm"].item() - want) <= 5 * R.U * want
+    nuq.adamw(lst, lr=R.LR, control=control, seed=77)
+    for p, a, b in zip(parts, before, read()):
+        _check([a], [b], [0.1], 3, bits, seed=77, first=p.start)
+
+
 def test_lists_refuse_what_does_not_fit():
     torch, nuq = require_cuda()
     z = lambda n, dtype=torch.float32: torch.zeros(n, dtype=dtype, device="cuda")  # noqa: E731
@@ -501,8 +536,8 @@ def test_lists_refuse_what_does_not_fit():
     lst, control = nuq.tensors([g], [w], [m], [v]), nuq.step_control()
     nan, inf = float("nan"), float("inf")
     for kw in (dict(lr=nan), dict(lr=-1.0), dict(lr=inf), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=nan), dict(eps=-1e-8), dict(eps=nan),
-               dict(scale=nan), dict(scale=inf), dict(step=0)):
-        with pytest.raises(nuq.NuqError):
+               dict(scale=nan), dict(scale=inf), dict(step=0), dict(step=-1), dict(step=1 << 64)):
+        with pytest.raises((nuq.NuqError, ValueError)):
             nuq.adamw(lst, **{"lr": 0.1, "step": 1, **kw})
     for kw in (dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=nan), dict(scale=inf), dict(scale=nan)):
         with pytest.raises(nuq.NuqError):

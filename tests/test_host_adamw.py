@@ -75,7 +75,7 @@ def test_adamw_refuses_a_tensor(lib, kw):
     assert not _launches(lib)
 
 
-@pytest.mark.parametrize("kw", [dict(lr=NAN), dict(lr=-1e-9), dict(lr=INF), dict(lr=1e39), dict(beta1=1.0), dict(beta1=-0.5), dict(beta1=NAN), dict(beta2=1.0), dict(beta2=NAN),
+@pytest.mark.parametrize("kw", [dict(lr=NAN), dict(lr=-1e-9), dict(lr=INF), dict(lr=1e13), dict(beta1=1.0), dict(beta1=-0.5), dict(beta1=NAN), dict(beta2=1.0), dict(beta2=NAN),
                                 dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(scale=NAN), dict(scale=INF), dict(scale=-INF), dict(step=0)])
 def test_adamw_refuses_constants(lib, kw):
     assert lib.nuq_adamw(_array(_tensor()), 1, _config(**kw), None, STREAM) == -1
