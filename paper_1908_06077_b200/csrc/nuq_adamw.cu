@@ -9,6 +9,7 @@
 
 #include "../../include/nuq.h"
 #include "nuq_adamw.cuh"
+#include "nuq_async.cuh"
 #include "nuq_launch.h"
 
 namespace nuq {
@@ -340,6 +341,16 @@ __device__ __forceinline__ void stage_in(T* shared, const T* from, uint32_t left
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i) shared[32u * i + lane_id()] = x[i];
 }
+// (four bytes at a time past the registers; the warp waits for its copies before it meets)
+template <bool WHOLE>
+__device__ __forceinline__ void stage_in(float* shared, const float* from, uint32_t left) {
+    const uint32_t to = smem_u32(shared) + 4u * lane_id();
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+        if (WHOLE || 32u * i + lane_id() < left) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 128u * i), "l"(from + 32u * i + lane_id()) : "memory");
+        else shared[32u * i + lane_id()] = 0.0f;
+    }
+}
 template <bool WHOLE, class T>
 __device__ __forceinline__ void stage_out(T* to, const T* shared, uint32_t left) {
 #pragma unroll
@@ -375,6 +386,7 @@ __device__ __forceinline__ void step_part8(const StepTensor& t, const AdamwParam
         stage_in<WHOLE>(s.m, tm, left);
         stage_in<WHOLE>(s.v, tv, left);
     }
+    asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
     __syncwarp();
 #pragma unroll
     for (uint32_t q = 0; q < 2; ++q) {
