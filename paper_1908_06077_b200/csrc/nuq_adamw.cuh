@@ -63,7 +63,7 @@ __device__ __forceinline__ AdamwFactors adamw_factors(const AdamwParams& P) {
 // the same number for whoever computes it from the formula in fp32.
 // (One element at a time: two in a register pair take half the instructions, but those run on one of the two multiply-add pipes
 // only, the one that the integer products of the random bits need, and their constants have to be moved to registers first.
-// 2.7 x 10^8 elements with 8-bit states 836 us in pairs, 802 us so, before both got faster otherwise.)
+// 2^28 elements with 8-bit states: in pairs 836 us, so 802, both before the other steps.)
 __device__ __forceinline__ float moment1(const AdamwParams& P, float g, float m) { return __fadd_rn(__fmul_rn(m, P.beta1), __fmul_rn(g, P.rest1)); }
 __device__ __forceinline__ float moment2(const AdamwParams& P, float g, float v) { return __fadd_rn(__fmul_rn(v, P.beta2), __fmul_rn(__fmul_rn(g, g), P.rest2)); }
 
