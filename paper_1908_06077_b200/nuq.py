@@ -243,6 +243,9 @@ def decode_update(streams, d, bucket, s, w, yl=None, alpha=1.0, mu=0.0, l=0.0, a
 
 _GRADS = {torch.float32: GRAD_F32, torch.bfloat16: GRAD_BF16, torch.float16: GRAD_F16}
 _COPIES = {torch.bfloat16: COPY_BF16, torch.float16: COPY_F16}
+_STATES = {torch.float32: STATES_F32, torch.uint8: STATES_8BIT}
+_F32 = (torch.float32,)
+_ITEM = {torch.float32: 4, torch.bfloat16: 2, torch.float16: 2, torch.uint8: 1}
 
 
 class Tensors:
@@ -267,7 +270,7 @@ def tensors(g, w=None, m=None, v=None, scales=None, copy=None, weight_decay=0.0)
     Raises ValueError where shapes, types, devices or alignment do not fit, or where written memory is given twice."""
     g = list(g)
     count = len(g)
-    lists = {"w": w, "m": m, "v": v, "scales": scales, "copy": copy}
+    lists = {"g": g, "w": w, "m": m, "v": v, "scales": scales, "copy": copy}
     for name, x in lists.items():
         x = lists[name] = [None] * count if x is None else list(x)
         if len(x) != count:
@@ -278,44 +281,49 @@ def tensors(g, w=None, m=None, v=None, scales=None, copy=None, weight_decay=0.0)
     states = w is not None
     if not states and any(x is not None for x in (m, v, scales, copy)):
         raise ValueError("states or copies without parameters")
-    array, device, written, read = (_Tensor * count)(), None, [], []
+    device = g[0].device if count and isinstance(g[0], torch.Tensor) else None
+    on = -1 if device is None or device.type != "cuda" else device.index
+    rows, spans = [], []                                    # the C array, eight words a tensor; what memory holds what
 
-    def place(name, i, x, types, n, out=True):
-        if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous() or x.dtype not in types or x.numel() != n:
-            raise ValueError(f"{name}[{i}]: a contiguous CUDA tensor of {n} elements, {' or '.join(map(str, types))}, is wanted")
-        if x.device != device:
-            raise ValueError(f"{name}[{i}]: on {x.device}, the first gradient is on {device}")
+    def place(name, i, types, n, writes=True):
+        x = lists[name][i]
+        if not isinstance(x, torch.Tensor) or x.dtype not in types or x.numel() != n or not x.is_contiguous() or on < 0 or x.get_device() != on:
+            raise ValueError(f"{name}[{i}]: a contiguous tensor of {n} elements, {' or '.join(map(str, types))}, on the CUDA device of the first gradient is wanted")
         p = x.data_ptr()
         if n:
-            (written if out else read).append((p, p + n * x.element_size(), f"{name}[{i}]"))
+            spans.append((p, p + n * _ITEM[x.dtype], writes, name, i))
         return p
 
     for i, x in enumerate(g):
-        if device is None and isinstance(x, torch.Tensor):
-            device = x.device
         n = x.numel() if isinstance(x, torch.Tensor) else 0
-        t = array[i]
-        t.g, t.n, t.weight_decay = place("g", i, x, tuple(_GRADS), n, False), n, decays[i]
-        t.types = _GRADS[x.dtype]
-        if not states:
-            continue
-        t.w = place("w", i, lists["w"][i], (torch.float32,), n)
-        t.m = place("m", i, lists["m"][i], (torch.float32, torch.uint8), n)
-        t.v = place("v", i, lists["v"][i], (lists["m"][i].dtype,), n)
-        if lists["m"][i].dtype == torch.uint8:
-            t.types |= STATES_8BIT
-            t.scales = place("scales", i, lists["scales"][i], (torch.float32,), 2 * -(-n // STATE_BLOCK))
-            if t.scales and t.scales % 8:
-                raise ValueError(f"scales[{i}]: 8-byte alignment is wanted")
-        if lists["copy"][i] is not None:
-            t.copy = place("copy", i, lists["copy"][i], tuple(_COPIES), n)
-            t.types |= _COPIES[lists["copy"][i].dtype]
-    ends = {True: (0, ""), False: (0, "")}                  # of what is written, of what is read (that may be given twice)
-    for a, b, name, writes in sorted([x + (True,) for x in written] + [x + (False,) for x in read]):
-        for end, other in (ends[True], ends[False] if writes else (0, "")):
-            if a < end:
-                raise ValueError(f"{name} and {other} overlap")
-        ends[writes] = max(ends[writes], (b, name))
+        row = [place("g", i, _GRADS, n, False), 0, 0, 0, 0, 0, n, 0]
+        types = _GRADS[x.dtype]
+        if states:
+            row[1] = place("w", i, _F32, n)
+            row[3] = place("m", i, _STATES, n)
+            kind = lists["m"][i].dtype
+            row[4] = place("v", i, (kind,), n)
+            types |= _STATES[kind]
+            if kind is torch.uint8:
+                row[5] = place("scales", i, _F32, 2 * -(-n // STATE_BLOCK))
+                if row[5] % 8:
+                    raise ValueError(f"scales[{i}]: 8-byte alignment is wanted")
+            if lists["copy"][i] is not None:
+                row[2] = place("copy", i, _COPIES, n)
+                types |= _COPIES[lists["copy"][i].dtype]
+        row[7] = types << 32 | int.from_bytes(C.c_float(decays[i]), "little")
+        rows += row
+    written = read = (0, 0, False, "", 0)                   # the spans that reach furthest, of what is written and of what is read
+    for span in sorted(spans):
+        for other in (written, read) if span[2] else (written,):    # (gradients may be given twice)
+            if span[0] < other[1]:
+                raise ValueError(f"{span[3]}[{span[4]}] and {other[3]}[{other[4]}] overlap")
+        if span[2]:
+            written = span
+        elif span[1] > read[1]:
+            read = span
+    words = (C.c_uint64 * len(rows))(*rows)
+    array = (_Tensor * count).from_buffer(words)
     return Tensors(array, device, (g, lists), states)
 
 
