@@ -254,9 +254,10 @@ class Tensors:
 
     def __init__(self, array, device, kept, states):
         self.array, self.device, self.kept, self.states = array, device, kept, states
+        self.count, self.address = len(array), C.addressof(array)
 
     def __len__(self):
-        return len(self.array)
+        return self.count
 
 
 def tensors(g, w=None, m=None, v=None, scales=None, copy=None, weight_decay=0.0) -> Tensors:
@@ -344,9 +345,9 @@ def control_fields(control) -> dict:
 def _control(control, device):
     if control is None:
         return None
-    if not control.is_cuda or control.dtype != torch.int64 or not control.is_contiguous() or 8 * control.numel() < CONTROL_BYTES:
+    if not control.is_cuda or control.dtype is not torch.int64 or not control.is_contiguous() or 8 * control.numel() < CONTROL_BYTES:
         raise ValueError(f"control: a contiguous int64 CUDA tensor of {CONTROL_BYTES // 8} elements is wanted")
-    if device is not None and control.device != device:
+    if device is not None and control.get_device() != device.index:
         raise ValueError(f"control: on {control.device}, the tensors are on {device}")
     return control.data_ptr()
 
@@ -357,19 +358,19 @@ def _config(lr, beta1, beta2, eps, scale, step, seed):
     return _AdamwConfig(lr, beta1, beta2, eps, scale, step, seed & 0xFFFFFFFFFFFFFFFF)
 
 
-def _on_device(device, stream, call):
-    """call(raw stream) with `device` current (the stream, if none is given, is its current one)"""
-    if device is None or device.index == _current_device():
-        return call(_stream(stream))
-    with torch.cuda.device(device):
-        return call(_stream(stream))
+def _on_device(index, stream, function, *args):
+    """function(*args, raw stream) with device `index` current (the stream, if none is given, is its current one)"""
+    if index is None or index == _current_device():
+        return function(*args, _stream(stream))
+    with torch.cuda.device(index):
+        return function(*args, _stream(stream))
 
 
 def grad_norm(list_, control, max_norm=float("inf"), scale=1.0, stream=None):
     """The gradients' Euclidean norm, the factor that clips it to max_norm and the beginning of the next step, all into
     `control` (see control_fields).  list_: from `tensors`."""
     where = _control(control, list_.device)
-    rc = _on_device(control.device, stream, lambda s: _lib.nuq_grad_norm(list_.array, len(list_), scale, max_norm, where, s))
+    rc = _on_device(control.get_device(), stream, _lib.nuq_grad_norm, list_.address, list_.count, scale, max_norm, where)
     if rc != NUQ_OK:
         raise NuqError("nuq_grad_norm", rc)
     return control
@@ -381,7 +382,7 @@ def adamw(list_, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=0, scale=1.0, seed=0
         raise ValueError("a list of gradients alone")
     where = _control(control, list_.device)
     config = _config(lr, beta1, beta2, eps, scale, step, seed)
-    rc = _on_device(list_.device, stream, lambda s: _lib.nuq_adamw(list_.array, len(list_), C.byref(config), where, s))
+    rc = _on_device(list_.device and list_.device.index, stream, _lib.nuq_adamw, list_.address, list_.count, C.byref(config), where)
     if rc != NUQ_OK:
         raise NuqError("nuq_adamw", rc)
 
@@ -400,9 +401,9 @@ def decode_adamw(streams, d, bucket, s, w, m, v, lr, beta1=0.9, beta2=0.999, eps
     where = _control(control, w.device)
     config = _config(lr, beta1, beta2, eps, scale, step, 0)
     ptrs = _pointers(streams)
-    rc = _on_device(w.device, stream, lambda raw: _lib.nuq_decode_adamw(
-        ptrs, len(streams), d, bucket, s, likely, acc.data_ptr() if acc is not None else None, w.data_ptr(), m.data_ptr(),
-        v.data_ptr(), weight_decay, C.byref(config), where, raw))
+    rc = _on_device(w.get_device(), stream, _lib.nuq_decode_adamw, ptrs, len(streams), d, bucket, s, likely,
+                    acc.data_ptr() if acc is not None else None, w.data_ptr(), m.data_ptr(), v.data_ptr(), weight_decay,
+                    C.byref(config), where)
     if rc != NUQ_OK:
         raise NuqError("nuq_decode_adamw", rc)
     return w

@@ -479,6 +479,38 @@ def test_encoded_decoded_clipped_and_applied():
     _check(before, after, [0.01] * len(sizes), 1, 32, f["scale"].item())
 
 
+def test_a_training_loop_with_8_bit_states():
+    """sums of encoded gradients of a quadratic, clipped, states in 8 bits, weights of several shapes: as the README has it"""
+    torch, nuq = require_cuda()
+    shapes, K, bucket, s = [(64, 33), (33,), (7, 5, 3), (1,)], 2, 256, 4
+    sizes = [int(np.prod(x)) for x in shapes]
+    d = sum(sizes)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    weights = [torch.randn(x, generator=gen, device="cuda") for x in shapes]
+    copies = [w.to(torch.bfloat16) for w in weights]
+    states = [[torch.zeros(n, dtype=torch.uint8, device="cuda") for n in sizes] for _ in range(2)]
+    scales = [torch.zeros(2 * -(-n // nuq.STATE_BLOCK), device="cuda") for n in sizes]
+    total = torch.zeros(d, device="cuda")
+    parts = list(torch.split(total, sizes))
+    tensors = nuq.tensors(parts, weights, *states, scales=scales, copy=copies, weight_decay=[0.05 if w.dim() > 1 else 0.0 for w in weights])
+    control = nuq.step_control()
+    for step in range(1, 6):
+        flat = torch.cat([w.reshape(-1) for w in weights])
+        containers = [nuq.encode(flat + 0.1 * torch.randn(d, generator=gen, device="cuda"), bucket, s, seed=k, offset=step)[0] for k in range(K)]
+        nuq.decode_accumulate(containers, d, bucket, s, acc=total)
+        before = [{"g": g.cpu().numpy(), "w": w.reshape(-1).cpu().numpy(), "m": m.cpu().numpy(), "v": v.cpu().numpy(), "scales": c.cpu().numpy()}
+                  for g, w, m, v, c in zip(parts, weights, *states, scales)]
+        nuq.grad_norm(tensors, control, max_norm=1.0, scale=1.0 / K)
+        nuq.adamw(tensors, lr=R.LR, seed=7, control=control)
+        assert nuq.last_status() == 0
+        f = {k: x.item() for k, x in nuq.control_fields(control).items()}
+        want = np.sqrt(sum((x["g"].astype(np.float64) ** 2).sum() for x in before)) / K
+        assert f["step"] == step and abs(f["norm"] - want) <= 5 * R.U * want
+        after = [{"g": g.cpu().numpy(), "w": w.reshape(-1).cpu().numpy(), "copy": c16.float().reshape(-1).cpu().numpy(), "m": m.cpu().numpy(), "v": v.cpu().numpy(), "scales": c.cpu().numpy()}
+                 for g, w, c16, m, v, c in zip(parts, weights, copies, *states, scales)]
+        _check(before, after, [0.05, 0.0, 0.05, 0.0], step, 8, f["scale"], "bfloat16", 7)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_offsets_beyond_32_bits(bits):
     """a tensor of more than 2^32 elements: the elements on both sides of 2^32 and the last ones, and the norm of all"""

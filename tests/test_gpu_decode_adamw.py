@@ -92,6 +92,44 @@ def test_decode_adamw_matches_the_oracle_s_sum_and_the_formula(K, d, bucket, s, 
     _check(total, K, before, [_inside(b, d, n) for (b, _), n in zip(bufs, "wmv")], 5, 0.1, 0.5)
 
 
+@pytest.mark.parametrize("skew", [4, 8, 20])
+@pytest.mark.parametrize("K,mode", [(3, O.MODE_ERC), (8, O.MODE_FIXED)])
+def test_states_at_multiples_of_16_bytes(K, mode, skew):
+    """w, m, v and acc need 16 bytes' alignment only, each its own"""
+    torch, nuq = require_cuda()
+    d, bucket, s = 70_001, 1024, 4
+    outs, hosts = _streams(torch, nuq, d, bucket, s, O.make_flags(mode=mode), K)
+    total = O.decode_accumulate(hosts, d, bucket, s)[1]
+    before = _states(d, 3)
+    bufs = [torch.full((d + 64,), float("nan"), device="cuda") for _ in range(4)]
+    places = [b[k:k + d] for b, k in zip(bufs, (skew, 0, 4, skew + 4))]
+    for x, y in zip(places, before):
+        x.copy_(torch.from_numpy(y))
+    nuq.decode_adamw(outs, d, bucket, s, *places[:3], lr=R.LR, step=2, acc=places[3], likely=LIKELY[mode])
+    assert nuq.last_status() == 0
+    assert np.array_equal(places[3].cpu().numpy().view(np.uint32), total.view(np.uint32))
+    _check(total, K, before, [x.cpu().numpy() for x in places[:3]], 2, 0.0)
+    for b in bufs:
+        assert int(torch.isnan(b).sum()) == 64               # nothing else was written
+
+
+def test_steps_on_two_streams_at_once():
+    torch, nuq = require_cuda()
+    d, bucket, s, K = 300_001, 8192, 4, 4
+    work = []
+    for mode in (O.MODE_ERC, O.MODE_FIXED):
+        outs, hosts = _streams(torch, nuq, d, bucket, s, O.make_flags(mode=mode), K, seed=mode)
+        before = _states(d, mode)
+        work.append((mode, outs, O.decode_accumulate(hosts, d, bucket, s)[1], before, [torch.from_numpy(x).cuda() for x in before], torch.cuda.Stream(), nuq.step_control(mode + 3)))
+    torch.cuda.synchronize()
+    for mode, outs, _, _, state, stream, control in work:
+        nuq.grad_norm(nuq.tensors([]), control, scale=0.5, stream=stream)
+        nuq.decode_adamw(outs, d, bucket, s, *state, lr=R.LR, weight_decay=0.1, control=control, likely=LIKELY[mode], stream=stream)
+    for mode, _, total, before, state, stream, _ in work:
+        assert nuq.last_status(stream) == 0
+        _check(total, K, before, [x.cpu().numpy() for x in state], mode + 4, 0.1, 0.5)
+
+
 def test_streams_of_several_kinds():
     torch, nuq = require_cuda()
     d, bucket, s = 50_001, 1024, 4
