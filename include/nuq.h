@@ -254,7 +254,8 @@ typedef struct nuq_control {
  *   max_norm  > 0; infinity: no clipping
  *   control   device
  * Squares are added in fp32 by eights and beyond that in fp64, in an order that does not change, so equal
- * gradients in the same tensors give the same bits on the same kind of GPU.  May be captured into a graph.
+ * gradients in the same tensors (at the same alignment) give the same bits on the same kind of GPU.  May be captured
+ * into a graph.
  */
 nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale, float max_norm, nuq_control* control,
                          void* stream);
