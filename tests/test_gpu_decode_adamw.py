@@ -184,6 +184,33 @@ def test_states_that_are_zero_infinite_or_nan(mode):
     assert abs(after[0][2001] - w[2001]) == 0.0              # an infinite root: no step
 
 
+@pytest.mark.parametrize("mode", [O.MODE_ERC, O.MODE_FIXED])
+@pytest.mark.parametrize("K", [2, 9])
+def test_buckets_with_tiny_and_with_no_norms(mode, K):
+    """norms below 2^-100, infinite and NaN ones: the slow way through a unit, with the step behind it"""
+    torch, nuq = require_cuda()
+    d, bucket, s = 256 * 40 + 77, 256, 4
+    outs, hosts = [], []
+    for k in range(K):
+        g = _gradient(d, 50 + k)
+        g[512:2048] *= np.float32(1e-33)
+        if k == 1:
+            g[2600], g[5000] = np.inf, np.nan
+        out, bits = nuq.encode(torch.from_numpy(g).cuda(), bucket, s, O.make_flags(mode=mode), seed=k + 1)
+        outs.append(out)
+        hosts.append(out.cpu().numpy().view(np.uint32)[: int(bits.item()) // 32].copy())
+    assert nuq.last_status() == nuq.WARN_NONFINITE
+    rc, total = O.decode_accumulate(hosts, d, bucket, s)
+    assert rc == 0 and np.isfinite(total).all()
+    before = _states(d, 3)
+    bufs = [_guarded(torch, x) for x in before]
+    accbuf, acc = _guarded(torch, np.zeros(d, np.float32))
+    nuq.decode_adamw(outs, d, bucket, s, *(x for _, x in bufs), lr=R.LR, step=1, likely=LIKELY[mode], acc=acc)
+    assert nuq.last_status() == 0
+    assert np.array_equal(_inside(accbuf, d, "acc").view(np.uint32), total.view(np.uint32))
+    _check(total, K, before, [_inside(b, d, n) for (b, _), n in zip(bufs, "wmv")], 1, 0.0)
+
+
 def test_record_skips_counts_and_scales():
     torch, nuq = require_cuda()
     d, bucket, s, K = 20_003, 1024, 4, 3
