@@ -390,15 +390,15 @@ __device__ __forceinline__ void decode_fields(const Params& P, const StreamHead*
                     }
                 }
             } else if constexpr (kAdamw) {
+                Held8 held[2] = {};                         // the loads of two slots are on their way together
 #pragma unroll
-                for (uint32_t q0 = 0; q0 < kSlots; q0 += 2u) {                 // the loads of two slots are on their way together
-                    Held8 held[2] = {};
+                for (uint32_t q = 0; q < 2; ++q)
+                    if (q < slots) held[q] = load_step8(out, e0 + kSB * q, wide_states);
 #pragma unroll
-                    for (uint32_t i = 0; i < 2; ++i)
-                        if (q0 + i < slots) held[i] = load_step8(out, e0 + kSB * (q0 + i), wide_states);
-#pragma unroll
-                    for (uint32_t i = 0; i < 2; ++i)
-                        if (q0 + i < slots) step8(out, e0 + kSB * (q0 + i), sum[q0 + i], held[i], wide_states);
+                for (uint32_t q = 0; q < kSlots; ++q) {
+                    if (q >= slots) break;
+                    step8(out, e0 + kSB * q, sum[q], held[q & 1u], wide_states);
+                    if (q + 2u < slots) held[q & 1u] = load_step8(out, e0 + kSB * (q + 2u), wide_states);
                 }
             } else {
 #pragma unroll
