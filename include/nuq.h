@@ -273,7 +273,8 @@ nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale,
  *             element i of tensor j (its place in the array) takes word i & 3 of Philox4x32-10(key = seed,
  *             counter = (i >> 2 (two words), t, j)), the lower 16 bits for m, the upper ones for sqrt(v).
  *   control   device, or NULL.  If given t is its step, gradients are multiplied by its scale too, lr by its
- *             lr_factor; with skip set, or step 0, nothing is changed.
+ *             lr_factor; with skip set, with step 0, or as long as no nuq_grad_norm has written the record
+ *             (its scale is still 0), nothing is changed.
  * Calls keep no state and use no workspace; they may be captured into graphs (a captured step without a
  * control repeats the t of the capture) and run on several streams at once.
  */
@@ -298,7 +299,7 @@ nuq_status nuq_adamw(const nuq_tensor* tensors, uint32_t count, const nuq_adamw_
  *   acc      device, d floats, 16-byte aligned, or NULL: receives the sum as from nuq_decode_accumulate
  *   w, m, v  device, d floats each, 16-byte aligned; updated in place; no two of them and acc may overlap
  *   weight_decay, config, control   as for nuq_adamw (scale multiplies the mean; the seed is not looked at).
- *            With a control whose skip is set w, m and v stay, acc is written all the same.
+ *            With a control whose step is not taken w, m and v stay, acc is written all the same.
  * Clipping by the norm needs the whole sum first: nuq_decode_accumulate, nuq_grad_norm, nuq_adamw.
  * Errors and captures as for nuq_decode_update; the first call on a device uploads tables of its own.
  */

@@ -605,12 +605,13 @@ cudaError_t launch_adamw(const nuq_tensor* tensors, uint32_t count, const AdamwP
 // nuq_control and, behind its fields, the norm's scratch
 struct ControlRecord {
     nuq_control c;
+    uint32_t begun;          // 1: the norm has written c (its scale may be 0 all the same)
+    uint32_t arrived;        // CTAs whose sums are there
     double carried;          // sum of the launches before this one
-    uint32_t arrived, pad;   // CTAs whose sums are there
-    double pad2[3];
+    double pad[3];
     double sums[kNormMaxGrid];
 };
-static_assert(sizeof(nuq_control) == 24 && offsetof(ControlRecord, sums) == 64 && sizeof(ControlRecord) <= NUQ_CONTROL_BYTES, "the record");
+static_assert(sizeof(nuq_control) == 24 && offsetof(ControlRecord, begun) == 24 && offsetof(ControlRecord, sums) == 64 && sizeof(ControlRecord) <= NUQ_CONTROL_BYTES, "the record");
 
 // The sum of eight squares.  In fp32 unless they leave its range: seven roundings of relative size 2^-24 in sums that are
 // added up in fp64.
@@ -738,6 +739,7 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
     control->c.norm = norm;
     control->c.scale = norm > max_norm ? scale * __fdiv_rn(max_norm, norm) : scale;
     control->c.skip = fine ? 0u : 1u;
+    control->begun = 1u;
     if (fine) control->c.step += 1u;
 }
 

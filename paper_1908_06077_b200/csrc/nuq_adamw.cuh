@@ -46,7 +46,7 @@ __device__ __forceinline__ AdamwFactors adamw_factors(const AdamwParams& P) {
         f.t = a.x;
         f.scale = P.scale * __uint_as_float(a.w);
         f.lr_factor = __uint_as_float(b.x);
-        f.taken = b.y == 0u && step != 0u;
+        f.taken = b.y == 0u && step != 0u && (b.z != 0u || __uint_as_float(a.w) != 0.0f);      // (b.z: ControlRecord::begun)
         // 1 - beta^t = -expm1(t ln beta): no cancellation, a relative error of a few 2^-24 whatever t is
         const float t = (float)step;
         first = P.lr * f.lr_factor / -expm1f(t * P.log1);

@@ -329,7 +329,8 @@ def tensors(g, w=None, m=None, v=None, scales=None, copy=None, weight_decay=0.0)
 
 
 def step_control(step=0, device=None) -> torch.Tensor:
-    """A step's record on the device (nuq_control): an int64 CUDA tensor, steps taken set to `step`, the learning rate's factor to 1."""
+    """A step's record on the device (nuq_control): an int64 CUDA tensor, steps taken set to `step`, the learning rate's factor to 1.
+    grad_norm begins the next step; until it has, steps with the record change nothing."""
     control = torch.zeros(CONTROL_BYTES // 8, dtype=torch.int64, device="cuda" if device is None else device)
     control[0] = int(step)
     control.view(torch.float32)[4] = 1.0

@@ -575,3 +575,36 @@ def test_lists_refuse_what_does_not_fit():
         with pytest.raises(nuq.NuqError):
             nuq.grad_norm(lst, control, **kw)
     assert not w.any().item() and control[0].item() == 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_record_whose_step_no_norm_has_begun_changes_nothing(bits):
+    """a record with a number of steps and no scale, as step_control makes it, is not a step's: gradients were multiplied by 0"""
+    torch, nuq = require_cuda()
+    t, lst, decays = _list(torch, nuq, [1000, 257], bits=bits, seed=82)
+    control = nuq.step_control(999)
+    f = nuq.control_fields(control)
+    before = _read(t)
+    nuq.adamw(lst, lr=1.0, control=control, seed=3)
+    for a, b in zip(before, _read(t)):
+        assert all(np.array_equal(a[n], b[n]) for n in a)
+    nuq.grad_norm(lst, control)
+    nuq.adamw(lst, lr=R.LR, control=control, seed=3)
+    assert f["step"].item() == 1000
+    after = _read(t)
+    _check(before, after, decays, 1000, bits, seed=3)
+    # a scale of 0 that grad_norm has written is one: the moments decay
+    nuq.grad_norm(lst, control, scale=0.0)
+    nuq.adamw(lst, lr=R.LR, control=control, seed=4)
+    assert f["step"].item() == 1001 and f["scale"].item() == 0.0 and f["skip"].item() == 0
+    _check(after, _read(t), decays, 1001, bits, 0.0, seed=4)
+
+
+def test_a_record_with_a_scale_of_the_caller_s_own():
+    torch, nuq = require_cuda()
+    t, lst, decays = _list(torch, nuq, [1000], seed=83)
+    control = nuq.step_control(6)
+    nuq.control_fields(control)["scale"].fill_(0.25)
+    before = _read(t)
+    nuq.adamw(lst, lr=R.LR, control=control)
+    _check(before, _read(t), decays, 6, 32, 0.25)

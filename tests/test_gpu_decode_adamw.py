@@ -302,3 +302,23 @@ def test_decode_adamw_refuses_what_does_not_fit():
         with pytest.raises((ValueError, nuq.NuqError)):
             nuq.decode_adamw(outs, d, bucket, s, args.pop("w"), args.pop("m"), args.pop("v"), **args)
     assert not w.any().item()
+
+
+@pytest.mark.parametrize("mode", [O.MODE_ERC, O.MODE_FIXED])
+def test_a_record_whose_step_no_norm_has_begun(mode):
+    torch, nuq = require_cuda()
+    d, bucket, s, K = 20_003, 1024, 4, 3
+    outs, hosts = _streams(torch, nuq, d, bucket, s, O.make_flags(mode=mode), K)
+    total = O.decode_accumulate(hosts, d, bucket, s)[1]
+    before = _states(d, 3)
+    bufs = [_guarded(torch, x) for x in before]
+    accbuf, acc = _guarded(torch, np.zeros(d, np.float32))
+    control = nuq.step_control(999)
+    nuq.decode_adamw(outs, d, bucket, s, *(x for _, x in bufs), lr=R.LR, control=control, likely=LIKELY[mode], acc=acc)
+    assert nuq.last_status() == 0
+    for (b, _), x, n in zip(bufs, before, "wmv"):
+        assert np.array_equal(_inside(b, d, n), x)
+    assert np.array_equal(_inside(accbuf, d, "acc").view(np.uint32), total.view(np.uint32))
+    nuq.grad_norm(nuq.tensors([]), control)
+    nuq.decode_adamw(outs, d, bucket, s, *(x for _, x in bufs), lr=R.LR, control=control, likely=LIKELY[mode])
+    _check(total, K, before, [_inside(b, d, n) for (b, _), n in zip(bufs, "wmv")], 1000, 0.0)
