@@ -203,7 +203,7 @@ nuq_status nuq_decode_update(const void* const* streams, uint32_t K, uint64_t d,
  *            never rounded to 0.  The element's step itself takes m and v before they are rounded.  A
  *            value that is not finite is held as NaN (code 0x7f, 0xff), also where it was infinite.
  *            All zeros (codes and scales) are the state before the first step.
- *   weight_decay  of this tensor (0 for biases and the like), >= 0 and finite
+ *   weight_decay  of this tensor (0 for biases and the like), >= 0 and finite, lr weight_decay below 2^128 too
  * n = 0 is allowed (the pointers are not looked at then).  No two buffers that a call writes may overlap,
  * nor may g with one of them.
  */

@@ -692,15 +692,20 @@ nuq_status nuq_decode_update(const void* const* streams, uint32_t K, uint64_t d,
     return enqueue_decode(streams, K, d, bucket, s, acc, w, yl, alpha, mu, l, stream);
 }
 
+constexpr double kMostFloat = 0x1.fffffep127;
+
+// A decay that the step's fp32 factor lr weight_decay can hold.
+static bool decay_ok(float weight_decay, double lr) { return weight_decay >= 0.0f && (double)weight_decay <= kMostFloat && lr * (double)weight_decay <= kMostFloat; }
+
 // What a list of tensors has to satisfy; `norm`: only its gradients are looked at.
-static bool tensors_ok(const nuq_tensor* tensors, uint32_t count, bool norm) {
+static bool tensors_ok(const nuq_tensor* tensors, uint32_t count, bool norm, double lr) {
     if (count != 0u && !tensors) return false;
     auto off = [](const void* p, uintptr_t unit) { return !p || (reinterpret_cast<uintptr_t>(p) & (unit - 1u)) != 0u; };
     for (uint32_t i = 0; i < count; ++i) {
         const nuq_tensor& t = tensors[i];
         const uint32_t grad = t.types & 0xffu, copy = t.types & 0xff00u, states = t.types & 0xffff0000u;
         if (grad > NUQ_GRAD_F16 || copy > NUQ_COPY_F16 || states > NUQ_STATES_8BIT || t.n >= (1ull << 40)) return false;
-        if (!norm && !(t.weight_decay >= 0.0f && t.weight_decay <= 3.4028234e38f)) return false;
+        if (!norm && !decay_ok(t.weight_decay, lr)) return false;
         if (t.n == 0u) continue;
         if (off(t.g, grad == NUQ_GRAD_F32 ? 4u : 2u)) return false;
         if (norm) continue;
@@ -712,7 +717,7 @@ static bool tensors_ok(const nuq_tensor* tensors, uint32_t count, bool norm) {
 
 nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale, float max_norm, nuq_control* control, void* stream) {
     std::lock_guard<std::mutex> lock(g_mu);
-    if (!tensors_ok(tensors, count, true) || !control || (reinterpret_cast<uintptr_t>(control) & 15u)) return NUQ_ERR_INVALID_ARG;
+    if (!tensors_ok(tensors, count, true, 0.0) || !control || (reinterpret_cast<uintptr_t>(control) & 15u)) return NUQ_ERR_INVALID_ARG;
     if (!(scale >= -3.4028234e38f && scale <= 3.4028234e38f) || !(max_norm > 0.0f)) return NUQ_ERR_INVALID_ARG;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return NUQ_ERR_CUDA;
@@ -721,9 +726,8 @@ nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale,
 
 // The step's constants: formed in fp64, rounded once.  False for arguments out of range.
 static bool make_adamw(const nuq_adamw_config* c, const nuq_control* control, double divisor, AdamwParams* P) {
-    const double most = 3.4028234e38;
     if (!c || (reinterpret_cast<uintptr_t>(control) & 15u)) return false;
-    if (!(c->lr >= 0.0 && c->lr <= 0x1p40) || !(c->eps >= 0.0 && c->eps <= 0x1p100) || !(c->scale >= -most && c->scale <= most)) return false;
+    if (!(c->lr >= 0.0 && c->lr <= 0x1p40) || !(c->eps >= 0.0 && c->eps <= 0x1p100) || !(c->scale >= -kMostFloat && c->scale <= kMostFloat)) return false;
     if (!(c->beta1 >= 0.0 && c->beta1 < 1.0) || !(c->beta2 >= 0.0 && c->beta2 < 1.0)) return false;
     if (!control && c->step == 0u) return false;
     P->beta1 = (float)c->beta1;
@@ -750,7 +754,7 @@ static bool make_adamw(const nuq_adamw_config* c, const nuq_control* control, do
 nuq_status nuq_adamw(const nuq_tensor* tensors, uint32_t count, const nuq_adamw_config* config, const nuq_control* control, void* stream) {
     std::lock_guard<std::mutex> lock(g_mu);
     AdamwParams P;
-    if (!tensors_ok(tensors, count, false) || !make_adamw(config, control, 1.0, &P)) return NUQ_ERR_INVALID_ARG;
+    if (!make_adamw(config, control, 1.0, &P) || !tensors_ok(tensors, count, false, config->lr)) return NUQ_ERR_INVALID_ARG;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return NUQ_ERR_CUDA;
     return launch_adamw(tensors, count, P, config->lr, device_sms(dev), static_cast<cudaStream_t>(stream)) == cudaSuccess ? NUQ_OK : NUQ_ERR_CUDA;
@@ -762,10 +766,9 @@ nuq_status nuq_decode_adamw(const void* const* streams, uint32_t K, uint64_t d, 
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     auto off = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0u; };
     if (!w || !m || !v || off(w) || off(m) || off(v) || off(acc)) return NUQ_ERR_INVALID_ARG;
-    if (!(weight_decay >= 0.0f && weight_decay <= 3.4028234e38f)) return NUQ_ERR_INVALID_ARG;
     if (likely != NUQ_LIKELY_AS_KNOWN && ((likely & 0xff0000ffu) != 0u || ((likely >> 8) & 0xffu) > kLevelsTable || (likely >> 16) > kModeCoded)) return NUQ_ERR_INVALID_ARG;
     DecodeParamsOf<AdamwSum> P;
-    if (K < 1 || !make_adamw(config, control, (double)K, &P.sum.step)) return NUQ_ERR_INVALID_ARG;
+    if (K < 1 || !make_adamw(config, control, (double)K, &P.sum.step) || !decay_ok(weight_decay, config->lr)) return NUQ_ERR_INVALID_ARG;
     int dev = 0;
     const nuq_status st = prepare_decode(P, streams, K, d, bucket, s, likely, stream, g_adamw_token_tables_ready, upload_adamw_token_tables, &dev);
     if (st != NUQ_OK) return st;

@@ -201,3 +201,14 @@ def test_decode_adamw_in_a_capture_needs_a_call_before(lib):
     assert _decode(lib) == 0
     lib.fake_capture(1)
     assert _decode(lib, control=CONTROL, config=_config(step=0)) == 0
+
+
+@pytest.mark.parametrize("lr,decay,rc", [(2.0, 1e38, 0), (2.0, 3e38, -1), (2.0 ** 40, 2.0 ** 87, 0), (2.0 ** 40, 2.0 ** 88, -1), (0.0, 3.4e38, 0), (1e-3, 3.4e38, 0)])
+def test_a_decay_that_fp32_cannot_hold_is_refused(lib, lr, decay, rc):
+    """lr weight_decay is formed once for all of a tensor's elements: infinite, it would make NaN of every parameter that is 0"""
+    for n in (1000, 0):
+        assert lib.nuq_adamw(_array(_tensor(), _tensor(weight_decay=decay, n=n)), 2, _config(lr=lr), None, STREAM) == rc
+    assert lib.nuq_adamw(_array(_tensor(weight_decay=decay)), 1, _config(lr=lr), CONTROL, STREAM) == rc
+    assert len(_launches(lib)) == (0 if rc else 3)
+    assert _decode(lib, decay=decay, config=_config(lr=lr)) == rc
+    assert lib.nuq_grad_norm(_array(_tensor(weight_decay=decay)), 1, 1.0, 1.0, CONTROL, STREAM) == 0
