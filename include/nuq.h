@@ -240,7 +240,7 @@ typedef struct nuq_control {
     uint64_t step;           /* steps taken, the one that nuq_grad_norm has begun included          */
     float norm;              /* out: |scale| times the gradients' Euclidean norm                    */
     float scale;             /* out: what the step multiplies gradients by: scale min(1, max_norm / norm) */
-    float lr_factor;         /* the caller's: multiplies the learning rate                          */
+    float lr_factor;         /* the caller's: multiplies the learning rate; >= 0, at most 2^40 / lr */
     uint32_t skip;           /* out: 1 when norm is not finite; steps with this record change nothing then */
 } nuq_control;
 #define NUQ_CONTROL_BYTES 16384u
@@ -274,7 +274,7 @@ nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale,
  *             counter = (i >> 2 (two words), t, j)), the lower 16 bits for m, the upper ones for sqrt(v).
  *   control   device, or NULL.  If given t is its step, gradients are multiplied by its scale too, lr by its
  *             lr_factor; with skip set, with step 0, or as long as no nuq_grad_norm has written the record
- *             (its scale is still 0), nothing is changed.
+ *             (its scale is still 0), or with an lr_factor out of its range, nothing is changed.
  * Calls keep no state and use no workspace; they may be captured into graphs (a captured step without a
  * control repeats the t of the capture) and run on several streams at once.
  */

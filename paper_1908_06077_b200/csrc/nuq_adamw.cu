@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kStepThreads, KIND != kStates32 ? kStepCtas8 :
     const AdamwFactors f = adamw_factors(P);
     if (!f.taken) return;
     uint64_t e0 = (uint64_t)(tile - T.first[i]) * (kStepTile * rounds) + (threadIdx.x >> 5) * NUQ_STATE_BLOCK;
-    const float keep = 1.0f - f.lr_factor * t.decay;
+    const float keep = adamw_keep(f, t.decay);
     __shared__ Staged s_staged[BITS8 ? kStepThreads / 32u : 1u];
     Line line = {};
     if (BITS8) {

@@ -33,6 +33,7 @@ struct AdamwFactors {
     bool taken;
 };
 
+constexpr float kMostRate = 0x1p40f;             // the largest learning rate
 __device__ __forceinline__ AdamwFactors adamw_factors(const AdamwParams& P) {
     AdamwFactors f;
     float first = P.first, second = P.second;
@@ -46,10 +47,11 @@ __device__ __forceinline__ AdamwFactors adamw_factors(const AdamwParams& P) {
         f.t = a.x;
         f.scale = P.scale * __uint_as_float(a.w);
         f.lr_factor = __uint_as_float(b.x);
-        f.taken = b.y == 0u && step != 0u && (b.z != 0u || __uint_as_float(a.w) != 0.0f);      // (b.z: ControlRecord::begun)
+        const float lr = P.lr * f.lr_factor;
+        f.taken = f.lr_factor >= 0.0f && lr <= kMostRate && b.y == 0u && step != 0u && (b.z != 0u || __uint_as_float(a.w) != 0.0f);      // (b.z: ControlRecord::begun)
         // 1 - beta^t = -expm1(t ln beta): no cancellation, a relative error of a few 2^-24 whatever t is
         const float t = (float)step;
-        first = P.lr * f.lr_factor / -expm1f(t * P.log1);
+        first = lr / -expm1f(t * P.log1);
         second = 1.0f / sqrtf(-expm1f(t * P.log2));
     }
     // (a learning rate of 0, or as good as that: a denominator that is infinite also for a root of 0)
@@ -58,6 +60,9 @@ __device__ __forceinline__ AdamwFactors adamw_factors(const AdamwParams& P) {
     f.eps = moves ? P.eps / first : __uint_as_float(0x7f800000u);
     return f;
 }
+
+// What multiplies w.  decay: lr weight_decay, finite, as is the factor; their product need not be, and 0 stays 0 all the same.
+__device__ __forceinline__ float adamw_keep(const AdamwFactors& f, float decay) { return fmaxf(1.0f - f.lr_factor * decay, -0x1.fffffep127f); }
 
 // The moments of an element.  Each product is rounded before it is added, so that what is rounded to 8 bits afterwards is
 // the same number for whoever computes it from the formula in fp32.

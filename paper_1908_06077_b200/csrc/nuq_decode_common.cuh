@@ -83,7 +83,7 @@ __device__ __forceinline__ const float* step_vector(const AdamwSum& P, uint32_t 
 __device__ __forceinline__ bool stores_only(const AdamwSum&) { return false; }
 __device__ __forceinline__ void begin_step(const AdamwSum& P) {
     AdamwFactors f = adamw_factors(P.step);
-    f.lr_factor = 1.0f - f.lr_factor * P.decay;             // (what multiplies w)
+    f.lr_factor = adamw_keep(f, P.decay);                   // (what multiplies w)
     step_factors() = f;
 }
 struct AdamwHeld {

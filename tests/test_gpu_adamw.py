@@ -608,3 +608,41 @@ def test_a_record_with_a_scale_of_the_caller_s_own():
     before = _read(t)
     nuq.adamw(lst, lr=R.LR, control=control)
     _check(before, _read(t), decays, 6, 32, 0.25)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("factor", [-1.0, -1e-30, float("nan"), float("inf"), 2.0 ** 50])
+def test_a_learning_rate_s_factor_out_of_range_changes_nothing(bits, factor):
+    """a negative one would take the decay with the wrong sign, the others leave NaN or infinity in every parameter"""
+    torch, nuq = require_cuda()
+    t, lst, _ = _list(torch, nuq, [1000, 257], bits=bits, seed=84)
+    control = nuq.step_control(4)
+    before = _read(t)
+    nuq.grad_norm(lst, control)
+    nuq.control_fields(control)["lr_factor"].fill_(factor)
+    nuq.adamw(lst, lr=R.LR, control=control, seed=3)
+    for a, b in zip(before, _read(t)):
+        assert all(np.array_equal(a[n], b[n]) for n in a)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_largest_decays(bits):
+    """lr_factor = 0 moves no parameter, whatever the decay; a product of factor and decay that leaves fp32 leaves zeros zero"""
+    torch, nuq = require_cuda()
+    t, lst, decays = _list(torch, nuq, [1000, 257], bits=bits, seed=85, decays=[3e38, 1e30])
+    control = nuq.step_control(4)
+    f = nuq.control_fields(control)
+    f["lr_factor"].fill_(0.0)
+    before = _read(t)
+    nuq.grad_norm(lst, control)
+    nuq.adamw(lst, lr=1.0, control=control, seed=3)
+    after = _read(t)
+    _check(before, after, decays, 5, bits, seed=3, lr=0.0)
+    assert all(np.array_equal(a["w"], b["w"]) for a, b in zip(before, after))
+    for x in t:
+        x["w"].view.zero_()
+    f["lr_factor"].fill_(2.0)
+    before = _read(t)
+    nuq.grad_norm(lst, control)
+    nuq.adamw(lst, lr=1.0, control=control, seed=3)
+    _check(before, _read(t), [0.0, 0.0], 6, bits, seed=3, lr=2.0)
