@@ -230,6 +230,11 @@ def decode_accumulate(streams, d, bucket, s, acc=None, stream=None):
     return acc
 
 
+# Parameters are written through their addresses.  Autograd hears of it here, as of any write in place: a backward pass through
+# a graph that saved them before the step is an error, not a wrong gradient.  (A replayed graph passes this by.)
+_written = torch._C._increment_version
+
+
 def decode_update(streams, d, bucket, s, w, yl=None, alpha=1.0, mu=0.0, l=0.0, acc=None, stream=None):
     """w <- w - (alpha / K) sum_k DECODE(streams[k]), or the momentum rule with yl when mu != 0; in place."""
     ptrs = _pointers(streams)
@@ -238,6 +243,7 @@ def decode_update(streams, d, bucket, s, w, yl=None, alpha=1.0, mu=0.0, l=0.0, a
                                 alpha, mu, l, _stream(stream))
     if rc != NUQ_OK:
         raise NuqError("nuq_decode_update", rc)
+    _written((w,))
     return w
 
 
@@ -252,8 +258,8 @@ class Tensors:
     """A list of tensors as grad_norm and adamw take it (see `tensors`).  It keeps the tensors alive; their contents are
     looked at by the calls it is given to, so it serves step after step as long as the tensors stay where they are."""
 
-    def __init__(self, array, device, kept, states):
-        self.array, self.device, self.kept, self.states = array, device, kept, states
+    def __init__(self, array, device, kept, states, written):
+        self.array, self.device, self.kept, self.states, self.written = array, device, kept, states, written
         self.count, self.address = len(array), C.addressof(array)
 
     def __len__(self):
@@ -325,7 +331,9 @@ def tensors(g, w=None, m=None, v=None, scales=None, copy=None, weight_decay=0.0)
             read = span
     words = (C.c_uint64 * len(rows))(*rows)
     array = (_Tensor * count).from_buffer(words)
-    return Tensors(array, device, (g, lists), states)
+    # (a tensor and the parts of it share one version)
+    versions = {id(x): x for x in (y if y._base is None else y._base for y in (*lists["w"], *lists["copy"]) if y is not None)}
+    return Tensors(array, device, (g, lists), states, tuple(versions.values()))
 
 
 def step_control(step=0, device=None) -> torch.Tensor:
@@ -386,6 +394,7 @@ def adamw(list_, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=0, scale=1.0, seed=0
     rc = _on_device(list_.device and list_.device.index, stream, _lib.nuq_adamw, list_.address, list_.count, C.byref(config), where)
     if rc != NUQ_OK:
         raise NuqError("nuq_adamw", rc)
+    _written(list_.written)
 
 
 def decode_adamw(streams, d, bucket, s, w, m, v, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, step=0, scale=1.0,
@@ -407,6 +416,7 @@ def decode_adamw(streams, d, bucket, s, w, m, v, lr, beta1=0.9, beta2=0.999, eps
                     C.byref(config), where)
     if rc != NUQ_OK:
         raise NuqError("nuq_decode_adamw", rc)
+    _written((w,))
     return w
 
 

@@ -646,3 +646,35 @@ def test_the_largest_decays(bits):
     nuq.grad_norm(lst, control)
     nuq.adamw(lst, lr=1.0, control=control, seed=3)
     _check(before, _read(t), [0.0, 0.0], 6, bits, seed=3, lr=2.0)
+
+
+@pytest.mark.parametrize("which", ["w", "copy", "part of w"])
+def test_a_backward_pass_through_parameters_from_before_the_step_is_an_error(which):
+    """the step writes parameters through their addresses; autograd has to hear of it, or it takes the new ones for those it has saved"""
+    torch, nuq = require_cuda()
+    whole = torch.randn(600, device="cuda")
+    if which == "part of w":
+        whole.requires_grad_()
+        parts = list(torch.split(whole, [300, 300]))
+        w = [x.detach() for x in parts]
+    else:
+        w = [torch.randn(300, device="cuda", requires_grad=which == "w") for _ in range(2)]
+    copies = [x.detach().to(torch.bfloat16).requires_grad_(which == "copy") for x in w]
+    zeros = lambda: [torch.zeros(300, device="cuda") for _ in range(2)]  # noqa: E731
+    lst = nuq.tensors(zeros(), w, zeros(), zeros(), copy=copies)
+    loss = whole.square().sum() if which == "part of w" else sum(x.float().square().sum() if which == "w" else (x * x).sum() for x in (w if which == "w" else copies))
+    nuq.adamw(lst, lr=R.LR, step=1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    # and one from after it is as ever
+    x = whole if which == "part of w" else (w if which == "w" else copies)[0]
+    x.square().sum().backward()
+    assert torch.equal(x.grad, 2 * x.detach())
+
+
+def test_parameters_made_in_inference_mode():
+    torch, nuq = require_cuda()
+    with torch.inference_mode():
+        g, w, m, v = (torch.ones(300, device="cuda") for _ in range(4))
+    nuq.adamw(nuq.tensors([g], [w], [m], [v]), lr=0.5, step=1)
+    assert float(w.max()) < 1.0

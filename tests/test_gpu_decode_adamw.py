@@ -322,3 +322,21 @@ def test_a_record_whose_step_no_norm_has_begun(mode):
     nuq.grad_norm(nuq.tensors([]), control)
     nuq.decode_adamw(outs, d, bucket, s, *(x for _, x in bufs), lr=R.LR, control=control, likely=LIKELY[mode])
     _check(total, K, before, [_inside(b, d, n) for (b, _), n in zip(bufs, "wmv")], 1000, 0.0)
+
+
+@pytest.mark.parametrize("call", ["decode_adamw", "decode_update"])
+def test_a_backward_pass_through_parameters_from_before_the_step_is_an_error(call):
+    torch, nuq = require_cuda()
+    d, bucket, s = 5000, 256, 3
+    outs, _ = _streams(torch, nuq, d, bucket, s, 0, 3)
+    w = torch.randn(d, device="cuda", requires_grad=True)
+    m, v = torch.zeros(d, device="cuda"), torch.zeros(d, device="cuda")
+    loss = w.square().sum()
+    if call == "decode_adamw":
+        nuq.decode_adamw(outs, d, bucket, s, w, m, v, lr=R.LR, step=1)
+    else:
+        nuq.decode_update(outs, d, bucket, s, w, alpha=0.1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    w.square().sum().backward()
+    assert torch.equal(w.grad, 2 * w.detach())
