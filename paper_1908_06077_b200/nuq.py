@@ -255,8 +255,10 @@ _ITEM = {torch.float32: 4, torch.bfloat16: 2, torch.float16: 2, torch.uint8: 1}
 
 
 class Tensors:
-    """A list of tensors as grad_norm and adamw take it (see `tensors`).  It keeps the tensors alive; their contents are
-    looked at by the calls it is given to, so it serves step after step as long as the tensors stay where they are."""
+    """A list of tensors as grad_norm and adamw take it (see `tensors`).  It holds their addresses and keeps the tensors alive; their
+    contents are looked at by the calls it is given to.  So it serves step after step as long as the tensors stay where they are: a
+    gradient that is allocated anew in every step (zero_grad(set_to_none=True), decode_accumulate without acc) needs a new list
+    each time, the old one would go on with the old gradient."""
 
     def __init__(self, array, device, kept, states, written):
         self.array, self.device, self.kept, self.states, self.written = array, device, kept, states, written
