@@ -210,9 +210,13 @@ def encode_static(g: torch.Tensor, bucket, s, norm_kind=0, seed=0, offset=0, *, 
 _pointer_arrays = {}
 
 
-def _pointers(streams):
-    """the containers' addresses as a C array (copied by the call it is handed to)"""
+def _pointers(streams, *others):
+    """the containers' addresses as a C array (copied by the call it is handed to); others: what has to be on the same CUDA device"""
     n = len(streams)
+    index = others[0].get_device()
+    found = [t.get_device() for t in streams] + [x.get_device() for x in others if x is not None]
+    if index < 0 or found.count(index) != len(found):
+        raise ValueError("containers, sums and parameters: CUDA tensors on one device are wanted")
     array = _pointer_arrays.get(n)
     if array is None:
         array = _pointer_arrays[n] = C.c_void_p * n
@@ -223,7 +227,7 @@ def decode_accumulate(streams, d, bucket, s, acc=None, stream=None):
     """acc <- sum_k DECODE(streams[k]); acc is overwritten."""
     if acc is None:
         acc = torch.empty(d, dtype=torch.float32, device=streams[0].device)
-    ptrs = _pointers(streams)
+    ptrs = _pointers(streams, acc)
     rc = _lib.nuq_decode_accumulate(ptrs, len(streams), d, bucket, s, acc.data_ptr(), _stream(stream))
     if rc != NUQ_OK:
         raise NuqError("nuq_decode_accumulate", rc)
@@ -237,7 +241,7 @@ _written = torch._C._increment_version
 
 def decode_update(streams, d, bucket, s, w, yl=None, alpha=1.0, mu=0.0, l=0.0, acc=None, stream=None):
     """w <- w - (alpha / K) sum_k DECODE(streams[k]), or the momentum rule with yl when mu != 0; in place."""
-    ptrs = _pointers(streams)
+    ptrs = _pointers(streams, w, yl, acc)
     rc = _lib.nuq_decode_update(ptrs, len(streams), d, bucket, s, acc.data_ptr() if acc is not None else None,
                                 w.data_ptr(), yl.data_ptr() if yl is not None else None,
                                 alpha, mu, l, _stream(stream))
@@ -404,16 +408,17 @@ def decode_adamw(streams, d, bucket, s, w, m, v, lr, beta1=0.9, beta2=0.999, eps
     """An AdamW step with the mean of DECODE(streams[k]) as the gradient; w, m and v (float32, d elements) in place.
     step: its number, from 1 on, or `control`.  likely: what the streams most likely are, as encode was told (MODE_* | LEVELS_*);
     received containers are not known by their addresses."""
-    for name, x in (("w", w), ("m", m), ("v", v), ("acc", acc)):
-        if x is not None and not (x.is_cuda and x.dtype == torch.float32 and x.is_contiguous() and x.numel() == d and x.device == w.device):
+    index = w.get_device()
+    for name, x in (("w", w), ("m", m), ("v", v)) + ((("acc", acc),) if acc is not None else ()):
+        if x.get_device() != index or index < 0 or x.dtype is not torch.float32 or not x.is_contiguous() or x.numel() != d:
             raise ValueError(f"{name}: a contiguous float32 CUDA tensor of {d} elements is wanted, all on one device")
     places = sorted((x.data_ptr(), x.data_ptr() + 4 * d) for x in (w, m, v, acc) if x is not None)
     if any(a[1] > b[0] for a, b in zip(places, places[1:])):
         raise ValueError("w, m, v and acc overlap")
     where = _control(control, w.device)
     config = _config(lr, beta1, beta2, eps, scale, step, 0)
-    ptrs = _pointers(streams)
-    rc = _on_device(w.get_device(), stream, _lib.nuq_decode_adamw, ptrs, len(streams), d, bucket, s, likely,
+    ptrs = _pointers(streams, w)
+    rc = _on_device(index, stream, _lib.nuq_decode_adamw, ptrs, len(streams), d, bucket, s, likely,
                     acc.data_ptr() if acc is not None else None, w.data_ptr(), m.data_ptr(), v.data_ptr(), weight_decay,
                     C.byref(config), where)
     if rc != NUQ_OK:

@@ -340,3 +340,17 @@ def test_a_backward_pass_through_parameters_from_before_the_step_is_an_error(cal
         loss.backward()
     w.square().sum().backward()
     assert torch.equal(w.grad, 2 * w.detach())
+
+
+def test_containers_in_host_memory_are_refused():
+    torch, nuq = require_cuda()
+    d, bucket, s = 5000, 256, 3
+    outs, _ = _streams(torch, nuq, d, bucket, s, 0, 2)
+    mixed = [outs[0], outs[1].cpu()]
+    x = [torch.zeros(d, device="cuda") for _ in range(3)]
+    for bad in (lambda: nuq.decode_adamw(mixed, d, bucket, s, *x, lr=0.1, step=1), lambda: nuq.decode_update(mixed, d, bucket, s, x[0], acc=x[1]),
+                lambda: nuq.decode_update(outs, d, bucket, s, x[0], acc=x[1].cpu()), lambda: nuq.decode_accumulate(mixed, d, bucket, s, acc=x[0]),
+                lambda: nuq.decode_accumulate(mixed, d, bucket, s)):
+        with pytest.raises(ValueError):
+            bad()
+    assert not any(y.any().item() for y in x)

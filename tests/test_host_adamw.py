@@ -212,3 +212,36 @@ def test_a_decay_that_fp32_cannot_hold_is_refused(lib, lr, decay, rc):
     assert len(_launches(lib)) == (0 if rc else 3)
     assert _decode(lib, decay=decay, config=_config(lr=lr)) == rc
     assert lib.nuq_grad_norm(_array(_tensor(weight_decay=decay)), 1, 1.0, 1.0, CONTROL, STREAM) == 0
+
+
+# ---- the binding ----
+
+def test_containers_in_host_memory_are_refused():
+    """their addresses went to the kernels as they were"""
+    torch = pytest.importorskip("torch")
+    from paper_1908_06077_b200 import nuq
+    host = [torch.zeros(64, dtype=torch.int32)] * 2
+    x = [torch.zeros(256) for _ in range(4)]
+    for bad in (lambda: nuq.decode_accumulate(host, 256, 256, 3), lambda: nuq.decode_accumulate(host, 256, 256, 3, acc=x[0]),
+                lambda: nuq.decode_update(host, 256, 256, 3, x[0], acc=x[1]), lambda: nuq.decode_adamw(host, 256, 256, 3, *x[:3], lr=0.1, step=1)):
+        with pytest.raises(ValueError):
+            bad()
+
+
+def test_containers_on_another_device_are_refused():
+    from paper_1908_06077_b200 import nuq
+
+    class On:
+        def __init__(self, index):
+            self.index = index
+
+        def get_device(self):
+            return self.index
+
+        def data_ptr(self):
+            return 4096
+
+    assert list(nuq._pointers([On(1), On(1)], On(1), None, On(1))) == [4096, 4096]
+    for streams, others in (([On(0)], [On(1)]), ([On(1), On(0)], [On(1)]), ([On(1), On(-1)], [On(1)]), ([On(-1)], [On(-1)]), ([On(0)], [On(0), On(1)]), ([On(0)], [On(0), None, On(-1)])):
+        with pytest.raises(ValueError):
+            nuq._pointers(streams, *others)
