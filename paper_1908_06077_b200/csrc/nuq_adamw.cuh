@@ -73,8 +73,11 @@ __device__ __forceinline__ float moment1(const AdamwParams& P, float g, float m)
 __device__ __forceinline__ float moment2(const AdamwParams& P, float g, float v) { return __fadd_rn(__fmul_rn(v, P.beta2), __fmul_rn(__fmul_rn(g, g), P.rest2)); }
 
 // sqrt(v), correctly rounded for v from 2^-100 to the largest number: an estimate of 1 / sqrt(v) within a few units of its last place,
-// and one step of Newton's method for s^2 = v, whose remainder is exact in a fused operation (compared with __fsqrt_rn for
-// every such v).  Below, the remainder would be lost; 0 and infinity give NaN: those are the caller's to find.
+// and one step of Newton's method for s^2 = v, whose remainder v - s^2 is exact in a fused operation (P. Markstein, Computation
+// of elementary functions on the IBM RISC System/6000 processor, IBM J. Res. Dev. 34, 1990: the sum of s and the remainder's
+// part is within a little more than half a unit, so a wrong rounding needs a root next to the middle between two numbers).  That
+// it happens for no v rests on a comparison with __fsqrt_rn for every one of them, which the tests repeat.  Below, the remainder
+// would be lost; 0 and infinity give NaN: those are the caller's to find.
 constexpr float kLeastRoot = 0x1p-100f;
 __device__ __forceinline__ float ordinary_root(float v) {
     float y;
@@ -93,7 +96,8 @@ __device__ __forceinline__ float reciprocal_estimate(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// 1 / x, correctly rounded for x from 2^-100 to 2^126: the same, for 1 / y = x (compared with __frcp_rn for every such x)
+// 1 / x, correctly rounded for x from 2^-100 to 2^126: the same, for 1 / y = x.  By Markstein's theorem (there) an estimate within one
+// unit of its last place is enough, except perhaps for an x whose mantissa is all ones; here too the tests compare every x, with __frcp_rn.
 __device__ __forceinline__ float reciprocal(float x) {
     const float y = reciprocal_estimate(x);
     return __fmaf_rn(y, __fmaf_rn(-x, y, 1.0f), y);
