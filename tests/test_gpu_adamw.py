@@ -678,3 +678,56 @@ def test_parameters_made_in_inference_mode():
         g, w, m, v = (torch.ones(300, device="cuda") for _ in range(4))
     nuq.adamw(nuq.tensors([g], [w], [m], [v]), lr=0.5, step=1)
     assert float(w.max()) < 1.0
+
+
+@pytest.mark.parametrize("skew", [0, 1])
+@pytest.mark.parametrize("total,count", [(9_000_001, 4), (20_000_003, 7), (70_000_001, 23)])
+def test_long_lists_of_8_bit_states_are_stepped_like_their_tensors(total, count, skew):
+    """A warp of a long call takes several blocks one after the other (2, 4 and 16 here, where an SM has seven CTAs).  Each tensor
+    in a call of its own, with as many empty ones in front (the random bits go by the place in the list), is short enough for
+    one block to a warp: equal bits are wanted."""
+    torch, nuq = require_cuda()
+    rng = np.random.default_rng(total)
+    share = rng.uniform(0.2, 1.0, count)
+    sizes = [int((total - 3000) * x / share.sum()) for x in share]
+    sizes[count // 2] = 1531                                 # a short one between the others
+    assert max(sizes) < 2 * torch.cuda.get_device_properties(0).multi_processor_count * 7 * 4 * 1024
+    starts, end = [], skew
+    for n in sizes:
+        starts.append(end)
+        end = end + n + 3 if skew else (end + n + 63) // 64 * 64 + 64
+    blocks = [-(-n // R.BLOCK) for n in sizes]
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    g = torch.randn(end, generator=gen, device="cuda").to(torch.bfloat16)
+    first = {"w": torch.randn(end, generator=gen, device="cuda"), "copy": torch.zeros(end, dtype=torch.bfloat16, device="cuda"),
+             "m": torch.randint(0, 127, (end,), generator=gen, device="cuda").to(torch.uint8), "v": torch.randint(0, 127, (end,), generator=gen, device="cuda").to(torch.uint8),
+             "scales": torch.rand(2 * sum(blocks), generator=gen, device="cuda") / 448.0 + 1e-4}
+    one, each = ({k: x.clone() for k, x in first.items()} for _ in range(2))
+
+    def lists(x):
+        cut = lambda y: [y[a:a + n] for a, n in zip(starts, sizes)]  # noqa: E731
+        at = [2 * sum(blocks[:i]) for i in range(count)]
+        return cut(g), cut(x["w"]), cut(x["m"]), cut(x["v"]), [x["scales"][a:a + 2 * b] for a, b in zip(at, blocks)], cut(x["copy"])
+
+    def list_of(x, keep):
+        return nuq.tensors(*[[y[:0] if not keep(i) else y for i, y in enumerate(col)] for col in lists(x)[:4]],
+                           scales=[y[:0] if not keep(i) else y for i, y in enumerate(lists(x)[4])],
+                           copy=[y[:0] if not keep(i) else y for i, y in enumerate(lists(x)[5])], weight_decay=[0.1 * (i % 3) for i in range(count)])
+
+    nuq.adamw(list_of(one, lambda i: True), lr=R.LR, step=3, seed=5)
+    for j in range(count):
+        nuq.adamw(list_of(each, lambda i: i == j), lr=R.LR, step=3, seed=5)
+    for k in first:
+        assert not torch.equal(one[k], first[k]), k
+        assert torch.equal(one[k].view(torch.int32) if k in ("w", "scales") else one[k].view(torch.int16) if k == "copy" else one[k],
+                           each[k].view(torch.int32) if k in ("w", "scales") else each[k].view(torch.int16) if k == "copy" else each[k]), k
+    # the gaps are as they were, and two of the tensors are what the formula gives
+    inside = torch.zeros(end, dtype=torch.bool, device="cuda")
+    for a, n in zip(starts, sizes):
+        inside[a:a + n] = True
+    for k in ("w", "copy", "m", "v"):
+        assert torch.equal(one[k][~inside], first[k][~inside]), k
+    row = lambda x, i: {k: _numpy(y[i].cpu()) for k, y in zip(("g", "w", "m", "v", "scales", "copy"), lists(x))}  # noqa: E731
+    for i in (count // 2, int(np.argmin([n if n != 1531 else total for n in sizes]))):
+        nothing = [{k: np.zeros(0, y.dtype) for k, y in row(first, i).items()}] * i
+        _check(nothing + [row(first, i)], nothing + [row(one, i)], [0.1 * (j % 3) for j in range(i + 1)], 3, 8, copy="bfloat16", seed=5)
