@@ -731,3 +731,42 @@ def test_long_lists_of_8_bit_states_are_stepped_like_their_tensors(total, count,
     for i in (count // 2, int(np.argmin([n if n != 1531 else total for n in sizes]))):
         nothing = [{k: np.zeros(0, y.dtype) for k, y in row(first, i).items()}] * i
         _check(nothing + [row(first, i)], nothing + [row(one, i)], [0.1 * (j % 3) for j in range(i + 1)], 3, 8, copy="bfloat16", seed=5)
+
+
+def test_a_long_run_of_8_bit_states_with_gradients():
+    """8000 steps on normal gradients of constant size 1, beta2 = 0.999, beside the rounding rule in 64 bits with random numbers of
+    its own: both wander alike.  Where the states have settled, E v = 1 + E var / (1 - beta2), and a rounding's variance is at most
+    its spacing (an eighth of the root) times how far the root has moved against its block's scale in a step, on average no
+    more than 3/2 (1 - beta2) of it: v is at most 3/16 of itself too high.  Blocks are independent of each other, so a mean is
+    off by the spread of the blocks' means / sqrt(blocks); six times that is allowed for."""
+    torch, nuq = require_cuda()
+    blocks, steps = 256, 8000
+    n = blocks * R.BLOCK
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    g, w = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    m, v = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    scales = torch.zeros(2 * blocks, device="cuda")
+    lst = nuq.tensors([g], [w], [m], [v], scales=[scales])
+    root, mean = torch.zeros(n, dtype=torch.float64, device="cuda"), torch.zeros(n, dtype=torch.float64, device="cuda")
+    for t in range(1, steps + 1):
+        g.normal_(generator=gen)
+        nuq.adamw(lst, lr=R.LR, step=t, seed=5)
+        x = (R.BETA2 * root * root + (1.0 - R.BETA2) * g.double() ** 2).sqrt()
+        unit = (x.view(blocks, -1).amax(1) / 448.0).repeat_interleave(R.BLOCK)
+        spacing = torch.exp2(torch.floor(torch.log2((x / unit).clamp(min=2.0 ** -6))) - 3.0)
+        root = torch.floor(x / unit / spacing + torch.rand(n, generator=gen, device="cuda", dtype=torch.float64)) * spacing * unit
+        y = R.BETA1 * mean + (1.0 - R.BETA1) * g.double()
+        unit = (y.abs().view(blocks, -1).amax(1) / 448.0).repeat_interleave(R.BLOCK)
+        spacing = torch.exp2(torch.floor(torch.log2((y.abs() / unit).clamp(min=2.0 ** -6))) - 3.0)
+        mean = torch.floor(y / unit / spacing + torch.rand(n, generator=gen, device="cuda", dtype=torch.float64)) * spacing * unit
+    got = {"root": torch.from_numpy(R.held(v.cpu().numpy(), scales.cpu().numpy()[1::2])), "m": torch.from_numpy(R.held(m.cpu().numpy(), scales.cpu().numpy()[0::2]))}
+    want = {"root": root.cpu(), "m": mean.cpu()}
+    for name, power in (("root", 1), ("root", 2), ("m", 1), ("m", 2)):
+        a, b = ((x[name] ** power).view(blocks, -1).mean(1) for x in (got, want))
+        off = 6.0 * float(((a.var() + b.var()) / blocks).sqrt())
+        print(f"{name}^{power}: {float(a.mean()):.4f}, rule {float(b.mean()):.4f}, allowed {off:.4f}")
+        assert abs(float(a.mean() - b.mean())) <= off, (name, power)
+    a = (got["root"] ** 2).view(blocks, -1).mean(1)
+    off = 6.0 * float((a.var() / blocks).sqrt())
+    assert 1.0 - off <= float(a.mean()) <= 1.0 / (1.0 - 3.0 / 16.0) + off
+    print(f"sd of the root {float(got['root'].std()):.4f}, mean of v {float(a.mean()):.4f}")
