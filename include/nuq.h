@@ -204,7 +204,7 @@ nuq_status nuq_decode_update(const void* const* streams, uint32_t K, uint64_t d,
  *            value that is not finite is held as NaN (code 0x7f, 0xff), also where it was infinite.
  *            What is kept is the mean of m and of sqrt(v), not each element: in long runs with beta2 = 0.999 and
  *            gradients of constant size a root wanders about its value with a standard deviation of 17 % (fp32:
- *            1.6 %), and v, its square, is 5 % too high on average (3/16 at most).
+ *            1.6 %), and v, its square, is 5 % too high on average (3/16 of itself at most).
  *            All zeros (codes and scales) are the state before the first step.
  *   weight_decay  of this tensor (0 for biases and the like), >= 0 and finite, lr weight_decay below 2^128 too
  * n = 0 is allowed (the pointers are not looked at then).  No two buffers that a call writes may overlap,

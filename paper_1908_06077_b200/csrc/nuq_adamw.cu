@@ -558,9 +558,11 @@ static cudaError_t launch_kind(const nuq_tensor* tensors, uint32_t count, const 
     const uint32_t rounds = KIND == kStates32 || share <= 1u ? 1u : share < 16u ? (uint32_t)share : 16u;
     auto flush = [&] {
         if (T.count == 0u) return cudaSuccess;
-        // (a launch takes longer the more parameters it has: a small table for few tensors)
+        // (A launch takes longer the more parameters it has, 7 ns for a tensor's place: one tensor of 256 elements 3.1 us in a table
+        // of 16, 3.5 of 64, 4.9 of 256, 5.9 of 400.  So each table has four times the places of the one before.)
         const cudaError_t e = T.count <= 16u    ? launch_step<16u, KIND>(shortened<16u, StepTable<16u>>(T), P, rounds, stream)
-                              : T.count <= 176u ? launch_step<176u, KIND>(shortened<176u, StepTable<176u>>(T), P, rounds, stream)
+                              : T.count <= 64u  ? launch_step<64u, KIND>(shortened<64u, StepTable<64u>>(T), P, rounds, stream)
+                              : T.count <= 256u ? launch_step<256u, KIND>(shortened<256u, StepTable<256u>>(T), P, rounds, stream)
                                                 : launch_step<kStepMany, KIND>(T, P, rounds, stream);
         T.count = T.tiles = 0;
         return e;
@@ -767,6 +769,7 @@ cudaError_t launch_grad_norm(const nuq_tensor* tensors, uint32_t count, float sc
     bool begin = true;
     auto flush = [&](bool end) {
         ControlRecord* const record = reinterpret_cast<ControlRecord*>(control);
+        // (the largest table costs 1.1 us more than one of 256 places, that one 0.1 more than one of 32)
         const cudaError_t e = T.count <= 32u    ? launch_norm<32u>(T, record, scale, max_norm, begin, end, sms, stream)
                               : T.count <= 256u ? launch_norm<256u>(T, record, scale, max_norm, begin, end, sms, stream)
                                                 : launch_norm<kNormMany>(T, record, scale, max_norm, begin, end, sms, stream);

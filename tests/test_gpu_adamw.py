@@ -770,3 +770,14 @@ def test_a_long_run_of_8_bit_states_with_gradients():
     off = 6.0 * float((a.var() / blocks).sqrt())
     assert 1.0 - off <= float(a.mean()) <= 1.0 / (1.0 - 3.0 / 16.0) + off
     print(f"sd of the root {float(got['root'].std()):.4f}, mean of v {float(a.mean()):.4f}")
+
+
+@pytest.mark.parametrize("bits,skew", [(32, 0), (8, 0), (8, 1)])
+@pytest.mark.parametrize("count", [16, 17, 64, 65, 256, 257, 400])
+def test_tables_of_every_size(count, bits, skew):
+    """lists at the ends of the tables in which they travel"""
+    torch, nuq = require_cuda()
+    t, lst, decays = _list(torch, nuq, [1 + (53 * i) % 300 for i in range(count)], bits=bits, skew=skew, seed=count)
+    before = _read(t)
+    nuq.adamw(lst, lr=R.LR, step=5, seed=3)
+    _check(before, _read(t), decays, 5, bits, seed=3)
