@@ -7,7 +7,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnuq.so")
 SOURCES = ["nuq_api.cu", "nuq_encode.cu", "nuq_encode_fixed4.cu", "nuq_decode_chains.cu", "nuq_decode_adamw.cu", "nuq_adamw.cu"]
 OBJECTS = [os.path.join(HERE, f[:-3] + ".o") for f in SOURCES]          # compiled side by side, then linked
-HEADERS = ["nuq_common.cuh", "nuq_adamw.cuh", "nuq_pairs.cuh", "nuq_async.cuh", "nuq_encode_common.cuh", "nuq_decode_common.cuh", "nuq_decode_fields.cuh", "nuq_decode_chains.cuh", "nuq_launch.h", os.path.join("..", "..", "include", "nuq.h")]
+HEADERS = ["nuq_common.cuh", "nuq_adamw.cuh", "nuq_async.cuh", "nuq_encode_common.cuh", "nuq_decode_common.cuh", "nuq_decode_fields.cuh", "nuq_decode_chains.cuh", "nuq_launch.h", os.path.join("..", "..", "include", "nuq.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--fmad=false", "-Xcompiler", "-fPIC"]
 

@@ -114,7 +114,7 @@ struct DecodeCall {
     uint32_t likely_table;   // the table the call most likely needs (kTabErc, kTabUniform, kTabFields), or kTabCoded: none to prepare (a level code of the streams' own, or streams of several kinds)
     uint32_t likely_levels;  // ... and the level set of its fields (kTabFields)
     uint32_t let_next;       // token streams: the kernel behind may be launched early
-    float minus_zero;        // -0.0f, which the compiler must not know (see product2 in nuq_pairs.cuh)
+    float minus_zero;        // -0.0f, which the compiler must not know (see product2 in nuq_decode_common.cuh)
     Workspace* ws;
 };
 // Sum: SumParams, or AdamwSum of nuq_adamw.cuh
