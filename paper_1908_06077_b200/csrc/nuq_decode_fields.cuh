@@ -176,7 +176,7 @@ __device__ __forceinline__ void load8(float (&v)[8], const float* src) {
     asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(src));
 }
 // A lane's eight elements of the AdamW step.  wide: all arrays are at multiples of 32 bytes, so that whole sectors are moved (25.6 x 10^6
-// elements, K = 8, 4 bits: 123 us; in halves of sectors 137).
+// elements, K = 8, 4 bits: 124 us; in halves of sectors, arrays 16 bytes off, 131).
 struct Held8 {
     float w[8], m[8], v[8];
 };
@@ -222,8 +222,8 @@ __device__ __forceinline__ void step8(const AdamwSum& P, uint64_t e, const float
 // that two would; else product and sum are rounded one after the other.  Other norms (tiny ones; not finite ones, where an
 // element without a symbol has no product) take the slow way.
 // `mine`: the warp's shared memory (a multiple of 16).  `tables_ready`: the table of levels has been built, and all threads
-// have met since.
-template <uint32_t W, bool EXACT, class Params>
+// have met since.  CALLED: in a function of its own, see decode_fields_call.
+template <uint32_t W, bool EXACT, bool CALLED = false, class Params>
 __device__ __forceinline__ void decode_fields(const Params& P, const StreamHead* heads, unsigned char* table_memory, bool tables_ready, uint32_t mine) {
     constexpr uint32_t kWords = field_words(W), kSlots = field_slots(W), kPitch = field_pitch(W), kItem = kFieldStreams * kPitch;
     const Geometry& G = P.geo;
@@ -390,15 +390,19 @@ __device__ __forceinline__ void decode_fields(const Params& P, const StreamHead*
                     }
                 }
             } else if constexpr (kAdamw) {
-                Held8 held[2] = {};                         // the loads of two slots are on their way together
+                // The loads of two slots are on their way together; of one in a called function, which has too few registers for two
+                // (25.6 x 10^6 elements, K = 8, 4 bits: 130 us with one, 162 with two, words of its inner loop spilled;
+                // in a kernel 126 and 124).
+                constexpr uint32_t kAhead = CALLED ? 1u : 2u;
+                Held8 held[kAhead] = {};
 #pragma unroll
-                for (uint32_t q = 0; q < 2; ++q)
+                for (uint32_t q = 0; q < kAhead; ++q)
                     if (q < slots) held[q] = load_step8(out, e0 + kSB * q, wide_states);
 #pragma unroll
                 for (uint32_t q = 0; q < kSlots; ++q) {
                     if (q >= slots) break;
-                    step8(out, e0 + kSB * q, sum[q], held[q & 1u], wide_states);
-                    if (q + 2u < slots) held[q & 1u] = load_step8(out, e0 + kSB * (q + 2u), wide_states);
+                    step8(out, e0 + kSB * q, sum[q], held[q % kAhead], wide_states);
+                    if (q + kAhead < slots) held[q % kAhead] = load_step8(out, e0 + kSB * (q + kAhead), wide_states);
                 }
             } else {
 #pragma unroll
@@ -431,7 +435,7 @@ __device__ __forceinline__ void decode_fields(const Params& P, const StreamHead*
 // that: the same text is right where it is inlined and where one kernel calls it.)
 template <uint32_t W, bool EXACT, class Kernel, class Params>
 __device__ __noinline__ void decode_fields_call(const Params& P, const StreamHead* heads, unsigned char* table_memory, uint32_t mine) {
-    decode_fields<W, EXACT>(P, heads, table_memory, false, mine);
+    decode_fields<W, EXACT, true>(P, heads, table_memory, false, mine);
 }
 
 }  // namespace nuq
