@@ -615,8 +615,8 @@ struct ControlRecord {
 };
 static_assert(sizeof(nuq_control) == 24 && offsetof(ControlRecord, begun) == 24 && offsetof(ControlRecord, sums) == 64 && sizeof(ControlRecord) <= NUQ_CONTROL_BYTES, "the record");
 
-// The sum of eight squares.  In fp32 unless they leave its range: seven roundings of relative size 2^-24 in sums that are
-// added up in fp64.
+// The sum of eight squares.  In fp32 unless they leave its range: eight roundings of relative size 2^-24 (seven with 16-bit gradients, whose
+// squares are exact) in sums that are added up in fp64.
 __device__ __forceinline__ double eight_squares(const float (&x)[8]) {
     float p = 0.0f;
 #pragma unroll

@@ -443,8 +443,9 @@ __device__ __forceinline__ void add_block(const Params& P, const AddPass& A, uin
 #pragma unroll
             for (int h = 0; h < 2 * NB; ++h) *reinterpret_cast<float4*>(P.sum.acc + e + 128 * h) = value(h);
         } else {
-            // The loads of four steps are on their way together; of two with the AdamW step's three vectors (2.7 x 10^8 elements, K = 2: 1450
-            // us with four, 1397 with two; 25.6 x 10^6, K = 8: 138 and 132).
+            // The loads of four steps are on their way together; of two with the AdamW step's three vectors.  25.6 x 10^6 elements of normal
+            // gradients (1.11 bits each), K = 1, 2, 4, 8, in us: one 162, 138.5, 135, 139; two 149, 134.5, 129.5, 140; four 146, 137,
+            // 131, 143.  2.7 x 10^8 elements, K = 2: 1354, 1392, 1443 (so the longest calls would rather have one).
             constexpr int kAtOnce = NB == 1 || std::is_same<typename Params::SumType, AdamwSum>::value ? 2 : 4;
 #pragma unroll
             for (int h0 = 0; h0 < 2 * NB; h0 += kAtOnce) {
@@ -976,6 +977,8 @@ template <class Sum>
 using DecodeKernel = void (*)(DecodeParamsOf<Sum>);
 // (level tables and exponential levels: s + 2 of them; uniform levels: 2^s + 1, s <= 8)
 // With the AdamW step there are kernels for the paper's levels only: the others take the way through the kernels for token streams.
+// 25.6 x 10^6 elements, 4 bits, K = 2, 4, 8: exponential levels 106, 112, 125 us; uniform ones 108, 113, 128, level tables 115, 114,
+// 129 (11 to 18 % above what the bytes take at a copy's rate).
 template <class Sum>
 static DecodeKernel<Sum> fields_kernel(uint32_t s, uint32_t levelset) {
     if (levelset == kLevelsExp) return s <= 2u ? decode_fields_kernel<3, true, Sum> : s <= 6u ? decode_fields_kernel<4, true, Sum> : decode_fields_kernel<5, true, Sum>;
