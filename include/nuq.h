@@ -303,7 +303,9 @@ nuq_status nuq_adamw(const nuq_tensor* tensors, uint32_t count, const nuq_adamw_
  *   w, m, v  device, d floats each, 16-byte aligned; updated in place; no two of them and acc may overlap
  *   weight_decay, config, control   as for nuq_adamw (scale multiplies the mean; the seed is not looked at).
  *            With a control whose step is not taken w, m and v stay, acc is written all the same.
- * Clipping by the norm needs the whole sum first: nuq_decode_accumulate, nuq_grad_norm, nuq_adamw.
+ * All d elements are one tensor here: one weight_decay (a network's biases cannot be left without it), fp32 states, no copy in 16 bits.
+ * Where parts of the sum differ in that, and for clipping by the norm, which needs the whole sum first, there are
+ * nuq_decode_accumulate, nuq_grad_norm and nuq_adamw over the parts.
  * Errors and captures as for nuq_decode_update; the first call on a device uploads tables of its own.
  */
 #define NUQ_LIKELY_AS_KNOWN 0xffffffffu

@@ -6,7 +6,8 @@
 // of 8-bit moments, so that its largest magnitude is one warp reduction.
 //
 // Measured, of a copy's 6538 GB/s (2^28 elements, passes for half a second): fp32 moments 1158 us, 106 %; the norm of bf16
-// gradients 80.2 us, 102 %; 8-bit moments with bf16 gradients and copy 783 us, 84 %, in short bursts 720 to 750: that kernel
+// gradients 80.4 us, 102 %; 8-bit moments with bf16 gradients and copy 770 to 796 us from card to card, 83 to 86 %, in short bursts 720 to
+// 750: that kernel
 // issues 535 instructions for a warp's 256 elements (76 % of the issue slots, two for each of the 36 wide products of the random
 // bits; ALU pipe 47 %, multiply-add pipe 53 %), which take 515 us by themselves, and the clock falls under the load.
 #include <cuda_bf16.h>

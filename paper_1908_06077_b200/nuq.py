@@ -338,7 +338,11 @@ def tensors(g, w=None, m=None, v=None, scales=None, copy=None, weight_decay=0.0)
     words = (C.c_uint64 * len(rows))(*rows)
     array = (_Tensor * count).from_buffer(words)
     # (a tensor and the parts of it share one version)
-    versions = {id(x): x for x in (y if y._base is None else y._base for y in (*lists["w"], *lists["copy"]) if y is not None)}
+    versions = {}
+    for x in (*lists["w"], *lists["copy"]):
+        if x is not None:
+            base = x._base
+            versions[id(x if base is None else base)] = x
     return Tensors(array, device, (g, lists), states, tuple(versions.values()))
 
 
