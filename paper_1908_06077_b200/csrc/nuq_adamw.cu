@@ -608,13 +608,13 @@ cudaError_t launch_adamw(const nuq_tensor* tensors, uint32_t count, const AdamwP
 // nuq_control and, behind its fields, the norm's scratch
 struct ControlRecord {
     nuq_control c;
-    uint32_t begun;          // 1: the norm has written c (its scale may be 0 all the same)
-    uint32_t arrived;        // CTAs whose sums are there
     double carried;          // sum of the launches before this one
+    uint32_t arrived;        // CTAs whose sums are there
+    uint32_t begun;          // 1: the norm has written c (its scale may be 0 all the same)
     double pad[3];
     double sums[kNormMaxGrid];
 };
-static_assert(sizeof(nuq_control) == 24 && offsetof(ControlRecord, begun) == 24 && offsetof(ControlRecord, sums) == 64 && sizeof(ControlRecord) <= NUQ_CONTROL_BYTES, "the record");
+static_assert(sizeof(nuq_control) == 24 && offsetof(ControlRecord, begun) == 36 && offsetof(ControlRecord, sums) == 64 && sizeof(ControlRecord) <= NUQ_CONTROL_BYTES, "the record");
 
 // The sum of eight squares.  In fp32 unless they leave its range: eight roundings of relative size 2^-24 (seven with 16-bit gradients, whose
 // squares are exact) in sums that are added up in fp64.

@@ -43,12 +43,13 @@ __device__ __forceinline__ AdamwFactors adamw_factors(const AdamwParams& P) {
     f.taken = true;
     if (P.control != nullptr) {                  // (the record's fields by their places, see nuq_control)
         const uint4 a = *reinterpret_cast<const uint4*>(P.control), b = *(reinterpret_cast<const uint4*>(P.control) + 1);
+        const uint32_t begun = reinterpret_cast<const uint32_t*>(P.control)[9];                  // (ControlRecord::begun)
         const uint64_t step = (uint64_t)a.x | (uint64_t)a.y << 32;
         f.t = a.x;
         f.scale = P.scale * __uint_as_float(a.w);
         f.lr_factor = __uint_as_float(b.x);
         const float lr = P.lr * f.lr_factor;
-        f.taken = f.lr_factor >= 0.0f && lr <= kMostRate && b.y == 0u && step != 0u && (b.z != 0u || __uint_as_float(a.w) != 0.0f);      // (b.z: ControlRecord::begun)
+        f.taken = f.lr_factor >= 0.0f && lr <= kMostRate && b.y == 0u && step != 0u && (begun != 0u || __uint_as_float(a.w) != 0.0f);
         // 1 - beta^t = -expm1(t ln beta): no cancellation, a relative error of a few 2^-24 whatever t is
         const float t = (float)step;
         first = lr / -expm1f(t * P.log1);

@@ -781,3 +781,20 @@ def test_tables_of_every_size(count, bits, skew):
     before = _read(t)
     nuq.adamw(lst, lr=R.LR, step=5, seed=3)
     _check(before, _read(t), decays, 5, bits, seed=3)
+
+
+def test_a_record_kept_from_before_it_was_marked_as_begun():
+    """the norm's scratch has its old places: words 24 to 31 its carried sum, 32 the count of CTAs, 36 zero"""
+    torch, nuq = require_cuda()
+    t, lst, decays = _list(torch, nuq, [1000, 70_000], seed=86)
+    control = nuq.step_control(6)
+    control.view(torch.float64)[3] = 123.456
+    nuq.control_fields(control)["scale"].fill_(0.25)
+    before = _read(t)
+    nuq.adamw(lst, lr=R.LR, control=control)
+    after = _read(t)
+    _check(before, after, decays, 6, 32, 0.25)
+    nuq.grad_norm(lst, control)
+    nuq.adamw(lst, lr=R.LR, control=control)
+    assert control[0].item() == 7
+    _check(after, _read(t), decays, 7, 32)
