@@ -269,7 +269,7 @@ nuq_status nuq_grad_norm(const nuq_tensor* tensors, uint32_t count, float scale,
  *     w  = (1 - lr weight_decay) w - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * fp32 arithmetic; the factors are formed in fp64 and rounded once (with a control on the device in fp32).
  * The quotient is m / (sqrt(v) a + b) with a and b formed beforehand, by an estimate of the reciprocal: within
- * a few units of its last place; a denominator below 2^-126 counts as 0.
+ * a few units of its last place; a denominator below 2^-126 counts as 0, and so does lr / (1 - beta1^t) up to 2^-96.
  *   tensors   HOST array, copied at call time; states of both kinds may be mixed
  *   config    HOST; lr in [0, 2^40], eps in [0, 2^100], beta1 and beta2 in [0, 1), scale finite
  *             step: t, from 1 on (not looked at with a control); seed: of the roundings of 8-bit states:

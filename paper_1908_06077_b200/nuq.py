@@ -341,8 +341,8 @@ def tensors(g, w=None, m=None, v=None, scales=None, copy=None, weight_decay=0.0)
     versions = {}
     for x in (*lists["w"], *lists["copy"]):
         if x is not None:
-            base = x._base
-            versions[id(x if base is None else base)] = x
+            x = x if (base := x._base) is None else base
+            versions[id(x)] = x
     return Tensors(array, device, (g, lists), states, tuple(versions.values()))
 
 

@@ -798,3 +798,16 @@ def test_a_record_kept_from_before_it_was_marked_as_begun():
     nuq.adamw(lst, lr=R.LR, control=control)
     assert control[0].item() == 7
     _check(after, _read(t), decays, 7, 32)
+
+
+def test_autograd_hears_of_every_buffer_that_parameters_are_parts_of():
+    torch, nuq = require_cuda()
+    bases = [torch.zeros(40, device="cuda") for _ in range(20)]
+    w = [x[i:i + 10] for x in bases for i in (0, 10, 25)]
+    make = lambda dtype=torch.float32: [torch.zeros(10, dtype=dtype, device="cuda") for _ in w]  # noqa: E731
+    copies = make(torch.bfloat16)
+    lst = nuq.tensors(make(), w, make(), make(), copy=[x if i % 2 else None for i, x in enumerate(copies)])
+    versions = [x._version for x in (*bases, *w, *copies)]
+    nuq.adamw(lst, lr=R.LR, step=1)
+    assert all(x._version > a for x, a in zip((*bases, *w), versions))
+    assert [x._version > a for x, a in zip(copies, versions[80:])] == [i % 2 == 1 for i in range(60)]
